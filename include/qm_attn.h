@@ -1,5 +1,6 @@
 /*
- * qm_attn.h - fused scaled-dot-product attention forward for AMD MI355X (gfx950).
+ * qm_attn.h - fused scaled-dot-product attention forward for AMD MI355X (gfx950),
+ * and the operators around it that serve a model (from "Serving" on, at the end).
  *
  * The operation is the paper's statement of the attention problem (Background,
  * subsection "Attention Operators and acceleration"): for queries Q, keys K and
@@ -50,6 +51,7 @@
 #define QM_ATTN_H
 
 #include <hip/hip_runtime_api.h>
+#include <stddef.h>
 
 #ifdef __cplusplus
 extern "C" {
@@ -58,7 +60,8 @@ extern "C" {
 /* 16-bit storage types of q, k, v and o. */
 typedef enum {
   QM_F16 = 0,  /* IEEE binary16 */
-  QM_BF16 = 1  /* bfloat16 (top half of an IEEE binary32) */
+  QM_BF16 = 1, /* bfloat16 (top half of an IEEE binary32) */
+  QM_E4M3 = 2  /* cached keys and values only: OCP E4M3 codes with one scale per tensor */
 } qm_dtype_t;
 
 /* Memory layouts of q, k, v and o (the _layout entry points; lse is always [B][H][N]). */
@@ -86,7 +89,16 @@ enum {
   QM_ERR_UNSUPPORTED = -9, /* a pointer is not 16-byte aligned */
   QM_ERR_LAYOUT = -10,     /* layout is not QM_BHND or QM_BNHD, or QM_BNHD with
                               d_qk = 192 */
-  QM_ERR_TILE = -11        /* qm_attn_set_tile_rows: rows is not 0, 128 or 256 */
+  QM_ERR_TILE = -11,       /* qm_attn_set_tile_rows: rows is not 0, 128 or 256 */
+  QM_ERR_WINDOW = -12,     /* window is below 1 (qm_attn_decode: below 0), or sinks below 0 */
+  QM_ERR_PAGE = -13,       /* page_size is not a multiple of 16 from 16 to 65536, num_pages,
+                              table_cols or max_length is below 1, or a sequence's table or the
+                              cache is too large to address */
+  QM_ERR_ROTARY = -14,     /* rotary is not a multiple of 16 from 0 to d, its table is missing or
+                              (starts NULL) shorter than N, eps is negative, infinite or NaN, or
+                              interleaved is neither 0 nor 1 */
+  QM_ERR_STRIDE = -15,     /* a stride is negative or not a multiple of 8 elements */
+  QM_ERR_WORKSPACE = -16   /* workspace is NULL or smaller than the call needs */
 };
 
 /*
@@ -235,6 +247,30 @@ int qm_attn_fwd_fp8_layout(const void* q, const void* k, const void* v, void* o,
                            int layout);
 
 /*
+ * qm_attn_fwd_window - causal attention forward in which a query sees a sliding
+ * window of the latest keys and a few first keys that stay visible (attention
+ * sinks): key j is visible to query i iff
+ *
+ *     j <= i  and  (i - j < window  or  j < sinks).
+ *
+ * Every row sees at least its own key.  Key blocks that no row of a query block
+ * sees are neither loaded nor computed, so a call costs about
+ * N * (window + sinks) pairs.  lse is over the visible keys.
+ *
+ *   window         keys a query sees counting its own, at least 1; any value of
+ *                  N - sinks or more hides nothing and gives exactly the causal
+ *                  qm_attn_fwd_layout (byte-identical).
+ *   sinks          first keys of each sequence that all later queries see, 0 or
+ *                  more (QM_ERR_WINDOW otherwise).
+ *   all other arguments, the arithmetic, determinism and the status codes are
+ *   those of qm_attn_fwd_layout with causal = 1.  Both layouts give
+ *   byte-identical results.
+ */
+int qm_attn_fwd_window(const void* q, const void* k, const void* v, void* o, float* lse,
+                       int B, int H, int Hkv, int N, int d_qk, int d_v, float scale,
+                       int window, int sinks, hipStream_t stream, int dtype, int layout);
+
+/*
  * qm_attn_set_tile_rows - a tuning control: the query rows one workgroup
  * owns, for every later call in the process.
  *
@@ -259,6 +295,147 @@ int qm_attn_fwd_fp8_layout(const void* q, const void* k, const void* v, void* o,
  * threads may or may not apply to them.
  */
 int qm_attn_set_tile_rows(int rows);
+
+/*
+ * ---------------------------------------------------------------------------
+ * Serving: what makes the queries and keys that the calls above take, a paged
+ * cache of keys and values, and attention of new tokens over it.
+ *
+ * The cache is two arrays of pages, k_cache and v_cache, of `cache_layout`
+ *
+ *   QM_BHND  [num_pages][Hkv][page_size][d]
+ *   QM_BNHD  [num_pages][page_size][Hkv][d]
+ *
+ * and of `cache_dtype`: the call's own dtype, or QM_E4M3 codes.  Either way the
+ * real tensor is k_scale (v_scale) times what is stored.  page_table
+ * [B][table_cols] int32 holds each sequence's pages in order: token t of
+ * sequence b is row t % page_size of page page_table[b][t / page_size].
+ * page_size is a multiple of 16.  The table, lengths, starts and counts are device
+ * arrays that the host does not read; entries of the table past a sequence's
+ * tokens are never used.  A page number outside 0 .. num_pages - 1 among those in
+ * use is not followed: see each call for what it gives instead.
+ *
+ * The arrays of numbers (page_table, lengths, starts, counts) must be 4-byte
+ * aligned, all others 16-byte aligned.
+ */
+
+/*
+ * qm_qk_norm_rope - the norm of each query and key head and the rotation by its
+ * token's position, in one pass.  Per row x of d columns:
+ *
+ *   y_c = x_c w_c / sqrt(mean(x^2) + eps)     where the weight is given, else y = x;
+ *   pairs (a, b) of the first `rotary` columns, pair j at angle index j:
+ *     a' = a cos[p][j] - b sin[p][j],  b' = b cos[p][j] + a sin[p][j]
+ *   with p the token's position starts[b] + t, and pair j = columns
+ *   (j, j + rotary / 2), or with interleaved = 1 columns (2 j, 2 j + 1);
+ *
+ * in fp32, rounded once (to nearest even) into the output.
+ *
+ *   q, k         [in]  device, of `dtype`.  q_strides and k_strides (host arrays,
+ *                      read during the call) give the elements from one batch,
+ *                      token and head to the next, in this order: multiples of 8,
+ *                      0 or more, so q and k may be parts of one projection's
+ *                      output, in any order of dimensions; the d columns are
+ *                      contiguous.  NULL: contiguous, in `layout`.
+ *   q_out, k_out [out] device, contiguous, of `dtype` in `layout` (as
+ *                      qm_attn_fwd_layout takes them).  They overlap no input.
+ *   q_weight, k_weight   [in] device, [d] of `dtype`, or NULL.
+ *   cos, sin     [in]  device, [table_rows][rotary / 2] float32; not read when
+ *                      rotary is 0.
+ *   starts       [in]  device, [B] int32: the position of each sequence's first
+ *                      token, or NULL for 0.
+ *   counts       [in]  device, [B] int32: tokens that each sequence holds, or NULL
+ *                      for N.  Rows of a padded batch from there on are written as
+ *                      zeros, whatever their input holds.
+ *   d            64 or 128.       rotary   0, or a multiple of 16 up to d.
+ *   A token whose position is outside the table gets NaN rows.
+ *   Hkv need not divide H.
+ *   stream, errors, capture: as for the calls above (one kernel, nothing else).
+ */
+int qm_qk_norm_rope(const void* q, const void* k, void* q_out, void* k_out,
+                    const void* q_weight, const void* k_weight, const float* cos,
+                    const float* sin, const int* starts, const int* counts, int B, int H,
+                    int Hkv, int N, int d, int rotary, int table_rows, float eps,
+                    int interleaved, const long long* q_strides, const long long* k_strides,
+                    hipStream_t stream, int dtype, int layout);
+
+/*
+ * qm_qk_norm_rope_append - qm_qk_norm_rope, with the keys and the values v
+ * written to the cache: token t of sequence b to position starts[b] + t.
+ *
+ *   v            [in]  device, of `dtype`, Hkv heads, v_strides as for k.
+ *   k_out        [out] may be NULL: the keys then go to the cache only.
+ *   k_cache, v_cache   [in, out] device.  Stored is key / k_scale and value /
+ *                      v_scale (the quotient as a product with the fp32
+ *                      reciprocal), from the fp32 result, to nearest even; E4M3
+ *                      values beyond 448 become 448, NaN stays NaN.
+ *   starts       [in]  tokens that each sequence's cache holds so far (NULL: 0).
+ *   k_scale, v_scale   finite, with a finite reciprocal (QM_ERR_SCALE otherwise).
+ *   cos, sin, the weights and rotary = 0 are as above: without them keys are
+ *   stored as they are.
+ *   Rows past a sequence's count store nothing.  A token whose position is outside
+ *   the rotation's table or the page table, or whose page number is out of range,
+ *   is not stored.  Pages that hold a written position must belong to one sequence.
+ */
+int qm_qk_norm_rope_append(const void* q, const void* k, const void* v, void* q_out, void* k_out,
+                           void* k_cache, void* v_cache, const int* page_table,
+                           const void* q_weight, const void* k_weight, const float* cos,
+                           const float* sin, const int* starts, const int* counts, int B, int H,
+                           int Hkv, int N, int d, int rotary, int table_rows, float eps,
+                           int interleaved, int num_pages, int page_size, int table_cols,
+                           float k_scale, float v_scale, const long long* q_strides,
+                           const long long* k_strides, const long long* v_strides,
+                           hipStream_t stream, int dtype, int layout, int cache_dtype,
+                           int cache_layout);
+
+/*
+ * qm_attn_decode - attention of one new token per sequence over the cache.  Query
+ * head h of sequence b sees the cached tokens j < lengths[b] of key/value head
+ * h / (H / Hkv), and with window > 0 of those only
+ *
+ *     j >= lengths[b] - window  or  j < sinks
+ *
+ * (the last row of qm_attn_fwd_window on the same tokens; the new token's own key
+ * is already in the cache).
+ *
+ *   q            [in]  device, [B][H][d] of `dtype`.
+ *   o            [out] device, [B][H][d] of `dtype`.
+ *   lse          [out] device, [B][H] float32, over the visible scaled scores.
+ *   lengths      [in]  device, [B] int32: cached tokens of each sequence.  0: o is
+ *                      0 and lse -infinity.  Below 0, above max_length or beyond the
+ *                      page table, or with a page number out of range among the
+ *                      visible tokens' pages: that sequence's o and lse are NaN.
+ *   d            64 or 128.  H % Hkv == 0.
+ *   max_length   a bound on lengths that the host knows; the call's split of the
+ *                cache is chosen for it (and for the number of sequences), so a close
+ *                one is faster.
+ *   window       0: every cached token is visible.  sinks: 0 or more.
+ *   k_scale, v_scale   as given to qm_qk_norm_rope_append (finite).
+ *   workspace    [out] device, 16-byte aligned, at least as many bytes as
+ *                qm_attn_decode_workspace says (NULL where that is 0).  Its content
+ *                before the call does not matter, and after it is unspecified; calls
+ *                that may run at once must not share one.
+ *
+ * Arithmetic as in qm_attn_fwd (E4M3 codes are widened exactly; the probabilities
+ * are rounded to `dtype` before the second product).  What the cache holds in
+ * places that are not visible does not matter, NaN included.  Results are
+ * deterministic; a sequence's bytes may depend on B, max_length and the device's CU
+ * count within the rounding of fp32 sums.  One kernel is enqueued, or two.
+ */
+int qm_attn_decode(const void* q, const void* k_cache, const void* v_cache, void* o, float* lse,
+                   const int* page_table, const int* lengths, int B, int H, int Hkv, int d,
+                   int num_pages, int page_size, int table_cols, int max_length, float scale,
+                   float k_scale, float v_scale, int window, int sinks, void* workspace,
+                   size_t workspace_bytes, hipStream_t stream, int dtype, int cache_dtype,
+                   int cache_layout);
+
+/*
+ * qm_attn_decode_workspace - the workspace of a qm_attn_decode call with these
+ * arguments on the current device, in bytes, into *bytes (0: none).  max_length is
+ * cut to table_cols * page_size as there.  Returns a status.
+ */
+int qm_attn_decode_workspace(int B, int H, int Hkv, int d, int page_size, int table_cols,
+                             int max_length, int window, int sinks, size_t* bytes);
 
 /* qm_attn_strerror - a static, human-readable string for a status code. */
 const char* qm_attn_strerror(int status);

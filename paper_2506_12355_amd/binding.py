@@ -7,6 +7,7 @@ There is no fallback: if ``libqm_attn.so`` is missing, loading fails loudly.
 from __future__ import annotations
 
 import ctypes
+import operator
 import os
 import threading
 
@@ -35,6 +36,11 @@ QM_ERR_LAUNCH = -8
 QM_ERR_UNSUPPORTED = -9
 QM_ERR_LAYOUT = -10
 QM_ERR_TILE = -11
+QM_ERR_WINDOW = -12
+QM_ERR_PAGE = -13
+QM_ERR_ROTARY = -14
+QM_ERR_STRIDE = -15
+QM_ERR_WORKSPACE = -16
 
 _lib = None
 _lock = threading.Lock()
@@ -88,6 +94,23 @@ def _declare(lib: ctypes.CDLL) -> ctypes.CDLL:
         ctypes.c_void_p, ctypes.c_int,
     ]
     lib.qm_attn_fwd_fp8_layout.restype = ctypes.c_int
+    lib.qm_attn_fwd_window.argtypes = [
+        ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p,
+        ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_int,
+        ctypes.c_float, ctypes.c_int, ctypes.c_int, ctypes.c_void_p, ctypes.c_int, ctypes.c_int,
+    ]
+    lib.qm_attn_fwd_window.restype = ctypes.c_int
+    P, I, F = ctypes.c_void_p, ctypes.c_int, ctypes.c_float
+    lib.qm_qk_norm_rope.argtypes = [P] * 10 + [I] * 7 + [F, I] + [P] * 3 + [I] * 2
+    lib.qm_qk_norm_rope.restype = ctypes.c_int
+    lib.qm_qk_norm_rope_append.argtypes = (
+        [P] * 14 + [I] * 7 + [F] + [I] * 4 + [F] * 2 + [P] * 4 + [I] * 4)
+    lib.qm_qk_norm_rope_append.restype = ctypes.c_int
+    lib.qm_attn_decode.argtypes = (
+        [P] * 7 + [I] * 8 + [F] * 3 + [I] * 2 + [P, ctypes.c_size_t, P] + [I] * 3)
+    lib.qm_attn_decode.restype = ctypes.c_int
+    lib.qm_attn_decode_workspace.argtypes = [I] * 9 + [P]
+    lib.qm_attn_decode_workspace.restype = ctypes.c_int
     lib.qm_attn_set_tile_rows.argtypes = [ctypes.c_int]
     lib.qm_attn_set_tile_rows.restype = ctypes.c_int
     lib.qm_attn_strerror.argtypes = [ctypes.c_int]
@@ -269,20 +292,9 @@ def _dtype_code(t) -> int:
     raise TypeError(f"q, k, v must be float16 or bfloat16, not {t.dtype}")
 
 
-def fwd(q, k, v, causal: bool = False, scale: float | None = None, out=None, lse=None,
-        stream=None, layout: str = "bhnd"):
-    """Attention forward on torch tensors on a ROCm device.
-
-    q is [B, H, N, d]; k is [B, Hkv, N, d] and v [B, Hkv, N, dv] with Hkv
-    dividing H.  Hkv = H and dv = d: multi-head attention (``qm_attn_fwd``);
-    Hkv < H: grouped-query or multi-query attention (``qm_attn_fwd_gqa``);
-    dv < d (d = 192, dv = 128, Hkv = H): the MLA shape (``qm_attn_fwd_mla``).
-    With ``layout="bnhd"`` the tensors are [B, N, heads, width] instead (q
-    [B, N, H, d], k [B, N, Hkv, d], v [B, N, Hkv, dv], o [B, N, H, dv];
-    ``qm_attn_fwd_layout``).  Returns (o, lse): o of q's dtype, lse float32
-    [B, H, N] in either layout.  ``scale`` defaults to 1/sqrt(d) rounded to
-    float32.  ``stream`` defaults to the current stream of q's device.
-    """
+def _checked(q, k, v, scale, out, lse, layout):
+    """The checks that the 16-bit calls share.  Returns (the C arguments up to the
+    query heads, Hkv, N, d, dv, scale, dtype code, o, lse)."""
     import torch
 
     if layout not in ("bhnd", "bnhd"):
@@ -320,18 +332,69 @@ def fwd(q, k, v, causal: bool = False, scale: float | None = None, out=None, lse
             raise ValueError(f"out must be a contiguous {list(oshape)} tensor of q's dtype")
     lse = _lse(q, lse, B, H, N)
     _check_outputs_on(device, out, lse)
-    lib = load_library()
     args = (q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), lse.data_ptr(), B, H)
+    return args, Hkv, N, d, dv, scale, code, out, lse
+
+
+def fwd(q, k, v, causal: bool = False, scale: float | None = None, out=None, lse=None,
+        stream=None, layout: str = "bhnd"):
+    """Attention forward on torch tensors on a ROCm device.
+
+    q is [B, H, N, d]; k is [B, Hkv, N, d] and v [B, Hkv, N, dv] with Hkv
+    dividing H.  Hkv = H and dv = d: multi-head attention (``qm_attn_fwd``);
+    Hkv < H: grouped-query or multi-query attention (``qm_attn_fwd_gqa``);
+    dv < d (d = 192, dv = 128, Hkv = H): the MLA shape (``qm_attn_fwd_mla``).
+    With ``layout="bnhd"`` the tensors are [B, N, heads, width] instead (q
+    [B, N, H, d], k [B, N, Hkv, d], v [B, N, Hkv, dv], o [B, N, H, dv];
+    ``qm_attn_fwd_layout``).  Returns (o, lse): o of q's dtype, lse float32
+    [B, H, N] in either layout.  ``scale`` defaults to 1/sqrt(d) rounded to
+    float32.  ``stream`` defaults to the current stream of q's device.
+    """
+    args, Hkv, N, d, dv, scale, code, out, lse = _checked(q, k, v, scale, out, lse, layout)
+    lib, device = load_library(), q.device
     causal = 1 if causal else 0
-    if bnhd:
+    if layout == "bnhd":
         _enqueue(lib.qm_attn_fwd_layout, device, stream, args + (Hkv, N, d, dv, scale, causal),
                  (code, QM_BNHD))
     elif dv != d:
-        if Hkv != H:
+        if Hkv != args[6]:
             raise ValueError("unequal head dimensions need as many key/value heads as query heads")
         _enqueue(lib.qm_attn_fwd_mla, device, stream, args + (N, d, dv, scale, causal), (code,))
-    elif Hkv == H:
+    elif Hkv == args[6]:
         _enqueue(lib.qm_attn_fwd, device, stream, args + (N, d, scale, causal), (code,))
     else:
         _enqueue(lib.qm_attn_fwd_gqa, device, stream, args + (Hkv, N, d, scale, causal), (code,))
     return out, lse
+
+
+def fwd_window(q, k, v, window: int, sinks: int = 0, scale: float | None = None, out=None,
+               lse=None, stream=None, layout: str = "bhnd"):
+    """Causal attention forward with a sliding window: query i sees key j iff j <= i
+    and (i - j < ``window`` or j < ``sinks``), the first ``sinks`` keys staying
+    visible to every later query.  ``window`` counts the query's own key (at least
+    1); a window that reaches every key gives exactly ``fwd(causal=True)``.
+    Tensors, types, the other arguments and the results are those of :func:`fwd`
+    (``qm_attn_fwd_window``; key blocks that no query sees cost nothing)."""
+    args, Hkv, N, d, dv, scale, code, out, lse = _checked(q, k, v, scale, out, lse, layout)
+    _enqueue(load_library().qm_attn_fwd_window, q.device, stream,
+             args + (Hkv, N, d, dv, scale, _int32(window, "window"), _int32(sinks, "sinks")),
+             (code, QM_BNHD if layout == "bnhd" else QM_BHND))
+    return out, lse
+
+
+def _int32(x, name: str) -> int:
+    """x as a C int: a value past its range would wrap unseen (a window of 2^32 + 1
+    would be 1)."""
+    x = operator.index(x)
+    if not -2 ** 31 <= x < 2 ** 31:
+        raise ValueError(f"{name} must fit 32 bits, not {x}")
+    return x
+
+
+def qm_attn_fwd_window(q, k, v, o, lse, B, H, Hkv, N, d_qk, d_v, scale, window, sinks, stream,
+                       dtype, layout) -> int:
+    """The sliding-window C entry point with plain integers for pointers; returns
+    the status."""
+    return load_library().qm_attn_fwd_window(q, k, v, o, lse, int(B), int(H), int(Hkv), int(N),
+                                             int(d_qk), int(d_v), float(scale), int(window),
+                                             int(sinks), stream, int(dtype), int(layout))

@@ -26,7 +26,11 @@ LIB_PATH = os.path.join(PKG_DIR, LIB_NAME)
 DEBUG_LIB_PATH = os.path.join(PKG_DIR, "libqm_attn_debug.so")
 
 SOURCES = ["qm_attn.cpp", "attn_fwd_gfx950.hip", "attn_fwd_split_gfx950.hip",
-           "attn_fwd_rows128_gfx950.hip"]
+           "attn_fwd_rows128_gfx950.hip", "attn_fwd_window_gfx950.hip"]
+
+# The operators around the attention forward, in a folder of their own.  Their kernels
+# keep NaNs apart (an unusable position or page gives NaN rows, and E4M3 codes of NaN).
+SERVING_SOURCES = ["serving/qm_serving.cpp", "serving/norm_rope.hip", "serving/decode.hip"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950",
@@ -52,6 +56,8 @@ def hipcc() -> str:
 
 def compile_command(source: str, out_path: str, debug_sync: bool = False) -> list:
     flags = [f for f in HIPCC_FLAGS if f != "-shared"]
+    if source in SERVING_SOURCES:
+        flags = [f for f in flags if f not in ("-Xarch_device", "-fno-honor-nans")]
     return ([hipcc()] + flags + (["-DQM_DEBUG_SYNC"] if debug_sync else [])
             + ["-I", INCLUDE, "-I", CSRC, "-c", "-o", out_path, os.path.join(CSRC, source)])
 
@@ -84,8 +90,9 @@ def build(verbose: bool = False) -> str:
     with tempfile.TemporaryDirectory() as tmp:
         compiles, links = [], []
         for path, debug in ((LIB_PATH, False), (DEBUG_LIB_PATH, True)):
-            objects = [os.path.join(tmp, f"{s}.{int(debug)}.o") for s in SOURCES]
-            compiles += [compile_command(s, o, debug) for s, o in zip(SOURCES, objects)]
+            sources = SOURCES + SERVING_SOURCES
+            objects = [os.path.join(tmp, f"{s.replace('/', '_')}.{int(debug)}.o") for s in sources]
+            compiles += [compile_command(s, o, debug) for s, o in zip(sources, objects)]
             links.append(link_command(objects, path + f".tmp{os.getpid()}"))
         _run_all(compiles, verbose)
         _run_all(links, verbose)

@@ -174,6 +174,8 @@ struct KParams {
   float vscale;  // factor of O: 1, or the FP8 value scale
   int qmode;
   int layout;    // 0: q, k, v, o as [B][heads][N][width]; 1: as [B][N][heads][width]
+  int window;    // WINDOW: keys a query sees, its own among them (<= N)
+  int sinks;     // WINDOW: first keys that every later query sees too (<= N)
 };
 
 // 16-bit type traits: the MFMA and the fp32 -> 16-bit pack (round to nearest
@@ -422,7 +424,14 @@ enum LayoutSet : int { kBhndOnly = 0, kEitherLayout = 1, kBnhdOnly = 2 };
 // group; G > 1 groups share the workgroup's query rows, group g walking key
 // blocks g, g + G, g + 2 G, ... through K and V rings of its own, and the
 // groups' results are merged at the end.
-template <int DK, int DV, int DT, bool CAUSAL, int WAVES, int G, int LAYOUTS>
+//
+// WINDOW (with CAUSAL): key j is visible to query i iff j <= i and (j > i - window
+// or j < sinks).  The key loop then walks the blocks that hold first keys and the
+// blocks from the window of the tile's first row on, those between them left out:
+// step j is block j, or j + skip past the first keys' blocks.  A row may see nothing
+// in the first steps; it keeps m = -FLT_MAX and l = O = 0 through them (a masked
+// score's probability is 2^-inf = 0 against any m) until its own window begins.
+template <int DK, int DV, int DT, bool CAUSAL, int WAVES, int G, int LAYOUTS, bool WINDOW = false>
 __device__ __forceinline__ void attn_fwd_body(const KParams& p) {
   using OP = Ops<DT>;
   using Frag = typename OP::Frag;        // one MFMA A or B operand
@@ -434,6 +443,7 @@ __device__ __forceinline__ void attn_fwd_body(const KParams& p) {
   constexpr int NMT = DV / 32;           // GEMM-II M tiles
   constexpr int BM = 32 * WAVES;         // query rows per workgroup
   static_assert(LV::NG % WAVES == 0, "each wave issues whole load groups");
+  static_assert(!WINDOW || (CAUSAL && G == 1), "windows are causal, without key groups");
   constexpr int GPWV = LV::NG / WAVES;   // V direct loads per wave per block
   constexpr int RING = ring_depth<DK, DV, DT, WAVES, G>();
   // Deferred GEMM-II: with four-block rings, GEMM-II of block j can run in
@@ -506,8 +516,12 @@ __device__ __forceinline__ void attn_fwd_body(const KParams& p) {
   i32x4 rk, rv;        // K and V rows of the head
   Frag qf[NKS];        // Q: B operand of GEMM-I, resident for the whole key loop
   int nblk, nkv;       // key blocks of the query block; steps: blocks per group, rounded up
+  int nsink = 0, skip = 0;   // WINDOW: blocks of first keys, and blocks left out after them
   // the key block of this wave's group in step j
-  auto key_block = [&](int j) { return G > 1 ? j * G + kgrp : j; };
+  auto key_block = [&](int j) {
+    if constexpr (WINDOW) return j < nsink ? j : j + skip;
+    else return G > 1 ? j * G + kgrp : j;
+  };
 
   // ---- HBM -> LDS: this wave's load groups of one K or V block ----
   // LDS: RING K slots, then RING V slots, of one 64-key block each
@@ -574,6 +588,12 @@ __device__ __forceinline__ void attn_fwd_body(const KParams& p) {
     const int kv_end = CAUSAL ? min(N, (qb + 1) * BM) : N;
     nblk = (kv_end + kBN - 1) / kBN;
     nkv = (nblk + G - 1) / G;
+    if constexpr (WINDOW) {
+      const int first = max(0, qb * BM - p.window + 1) / kBN;   // the block of the first row's window
+      nsink = min(first, (p.sinks + kBN - 1) / kBN);
+      skip = first - nsink;
+      nkv = nblk - skip;
+    }
     // lane: query row, k-group (OP::KGB bytes of each k-step)
     const uint32_t q_off = (uint32_t)(qb * BM + wave * 32 + (lane & 31)) * rs_q +
                            (uint32_t)((lane >> 5) * OP::KGB);
@@ -806,14 +826,18 @@ __device__ __forceinline__ void attn_fwd_body(const KParams& p) {
       }
 
       // mask: keys past the end of the sequence, keys after the query (causal)
-      const bool need_mask = (j0 + kBN > N) || (CAUSAL && j0 + kBN - 1 > qw);
+      bool need_mask = (j0 + kBN > N) || (CAUSAL && j0 + kBN - 1 > qw);
+      // some key lies before some row's window and is no first key
+      if constexpr (WINDOW) need_mask |= j0 <= qw + 31 - p.window && j0 + kBN > p.sinks;
       if (need_mask) {
   #pragma unroll
         for (int kt = 0; kt < 2; ++kt) {
   #pragma unroll
           for (int r = 0; r < 16; ++r) {
             const int key = j0 + 32 * kt + 8 * (r / 4) + 4 * hi + (r % 4);
-            if (key >= N || (CAUSAL && key > qrow)) s[kt][r] = -INFINITY;
+            bool hidden = key >= N || (CAUSAL && key > qrow);
+            if constexpr (WINDOW) hidden |= key <= qrow - p.window && key >= p.sinks;
+            if (hidden) s[kt][r] = -INFINITY;
           }
         }
       }
@@ -997,7 +1021,7 @@ __device__ __forceinline__ void attn_fwd_body(const KParams& p) {
     // loads of the blocks after those, and takes every barrier.
     const int b_act = (qw >= N) ? 0 : (CAUSAL ? min(nblk, (qw + 31) / kBN + 1) : nblk);
     const int j_act =
-        G > 1 ? __builtin_amdgcn_readfirstlane((unsigned)(b_act - kgrp + G - 1) / G) : b_act;
+        WINDOW ? max(b_act - skip, 0) : G > 1 ? __builtin_amdgcn_readfirstlane((unsigned)(b_act - kgrp + G - 1) / G) : b_act;
     // The computed blocks run in one loop and the skipped ones in a second,
     // so that no block tests whether it computes; only the four-wave causal
     // d = 64 instance, at its register ceiling, keeps that test inside one
@@ -1282,15 +1306,17 @@ inline KParams make_params(const AttnArgs& a, int bm, int cus, int resident) {
   kp.group = a.H / a.Hkv;
   kp.nq = (a.N + bm - 1) / bm;
   const long long blocks = (long long)kp.nq * a.B * a.H;
-  kp.paired = a.causal && blocks > cus && (a.N > 2048 || blocks > resident);
+  kp.paired = a.causal && !a.window && blocks > cus && (a.N > 2048 || blocks > resident);
   kp.wg_per_head = kp.paired ? (kp.nq + 1) / 2 : kp.nq;
   kp.total = kp.wg_per_head * a.B * a.H;
-  kp.row = a.causal && !kp.paired && blocks > cus ? cus / kXcds : 0;
+  kp.row = a.causal && !a.window && !kp.paired && blocks > cus ? cus / kXcds : 0;
   kp.xcd_heads = (a.B * a.H) % kXcds ? 0 : a.B * a.H / kXcds;
   kp.c = a.c;
   kp.vscale = a.vscale;
   kp.qmode = a.qmode;
   kp.layout = a.layout;
+  kp.window = a.window;
+  kp.sinks = a.sinks;
   return kp;
 }
 

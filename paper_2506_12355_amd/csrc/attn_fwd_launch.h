@@ -34,6 +34,8 @@ struct AttnArgs {
   int qmode;    // QMode
   int layout;   // 0: [B][heads][N][width], 1: [B][N][heads][width] (q, k, v, o)
   int tile_rows;  // query rows per workgroup: 0 = chosen from the shape, 128 or 256
+  int window;   // 0, or (causal) the keys a query sees, its own among them, fewer than N
+  int sinks;    // with a window: first keys that every later query sees too
 };
 
 // Enqueues the kernel instance for (d, dv, dtype, causal, workgroup size, key
@@ -46,5 +48,8 @@ hipError_t launch_attn_fwd_split(const AttnArgs& a, int groups, hipStream_t stre
 
 // Enqueues a 128-row instance for 192-wide keys or the [B][N][heads][width] layout.
 hipError_t launch_attn_fwd_rows128(const AttnArgs& a, hipStream_t stream);
+
+// Enqueues an instance with a sliding window (a.window > 0, 16-bit types).
+hipError_t launch_attn_fwd_window(const AttnArgs& a, hipStream_t stream);
 
 }  // namespace qm

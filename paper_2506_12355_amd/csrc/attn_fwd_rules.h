@@ -93,6 +93,12 @@ inline int choose_waves(const AttnArgs& a, int cus) {
   return half_units(128, 14, 21) < half_units(256, 20, 40) ? 4 : 8;
 }
 
+// The same choice for a sliding window.
+inline int choose_window_waves(const AttnArgs& a, int cus) {
+  (void)cus;
+  return a.window > 2048 ? 8 : 4;
+}
+
 // Workgroups of a launch over `total` tiles: as many as are `resident` at once, each
 // walking tiles in turn (rounds of `resident` tiles), or one per tile.
 //

@@ -12,22 +12,13 @@
 #include <string.h>
 
 #include "attn_fwd_launch.h"
+#include "checks.h"
 
 namespace {
 
-bool overlaps(const void* a, size_t na, const void* b, size_t nb) {
-  const uintptr_t a0 = reinterpret_cast<uintptr_t>(a), b0 = reinterpret_cast<uintptr_t>(b);
-  return a0 < b0 + nb && b0 < a0 + na;
-}
-
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-
-// finite iff the exponent field is not all ones (independent of fast-math flags)
-bool finite_bits(float x) {
-  uint32_t u;
-  memcpy(&u, &x, sizeof(u));
-  return (u & 0x7F800000u) != 0x7F800000u;
-}
+using qm::aligned16;
+using qm::finite_bits;
+using qm::overlaps;
 
 constexpr int kFp8 = 2;   // internal dtype code: FP8 E4M3 inputs, bf16 output
 
@@ -40,7 +31,8 @@ std::atomic<int> g_tile_rows{0};
 // E4M3 codes scaled by qs, ks, vs, and o is bf16.
 int attn_fwd(const void* q, const void* k, const void* v, void* o, float* lse, int B, int H,
              int Hkv, int N, int d, int dv, float scale, int causal, hipStream_t stream,
-             int dtype, float qs = 1.0f, float ks = 1.0f, float vs = 1.0f, int layout = QM_BHND) {
+             int dtype, float qs = 1.0f, float ks = 1.0f, float vs = 1.0f, int layout = QM_BHND,
+             int window = 0, int sinks = 0) {
   if (!q || !k || !v || !o || !lse) return QM_ERR_NULL;
   if (B < 1 || H < 1 || N < 1 || Hkv < 1 || Hkv > H || H % Hkv != 0) return QM_ERR_SHAPE;
   if (!((d == 64 && dv == 64) || (d == 128 && dv == 128) || (d == 192 && dv == 128)))
@@ -120,6 +112,13 @@ int attn_fwd(const void* q, const void* k, const void* v, void* o, float* lse, i
   }
   a.layout = layout;
   a.tile_rows = g_tile_rows.load(std::memory_order_relaxed);
+  // a window that hides nothing is the causal mask
+  if (window > 0 && window < N - (sinks < N ? sinks : N)) {
+    a.window = window;
+    a.sinks = sinks;
+    return qm::launch_attn_fwd_window(a, stream) == hipSuccess ? QM_OK : QM_ERR_LAUNCH;
+  }
+  a.window = a.sinks = 0;
   return qm::launch_attn_fwd(a, stream) == hipSuccess ? QM_OK : QM_ERR_LAUNCH;
 }
 
@@ -170,6 +169,15 @@ extern "C" int qm_attn_fwd_fp8_layout(const void* q, const void* k, const void* 
                   k_scale, v_scale, layout);
 }
 
+extern "C" int qm_attn_fwd_window(const void* q, const void* k, const void* v, void* o,
+                                  float* lse, int B, int H, int Hkv, int N, int d_qk, int d_v,
+                                  float scale, int window, int sinks, hipStream_t stream,
+                                  int dtype, int layout) {
+  if (window < 1 || sinks < 0) return QM_ERR_WINDOW;
+  return attn_fwd(q, k, v, o, lse, B, H, Hkv, N, d_qk, d_v, scale, 1, stream,
+                  dtype == kFp8 ? -1 : dtype, 1.0f, 1.0f, 1.0f, layout, window, sinks);
+}
+
 extern "C" int qm_attn_set_tile_rows(int rows) {
   if (rows != 0 && rows != 128 && rows != 256) return QM_ERR_TILE;
   g_tile_rows.store(rows, std::memory_order_relaxed);
@@ -193,6 +201,14 @@ extern "C" const char* qm_attn_strerror(int status) {
     case QM_ERR_LAYOUT:
       return "layout must be QM_BHND (0), or QM_BNHD (1) with head dimension 64 or 128";
     case QM_ERR_TILE: return "tile rows must be 0 (chosen per call), 128 or 256";
+    case QM_ERR_WINDOW: return "a window must hold at least one key, and sinks be 0 or more";
+    case QM_ERR_PAGE:
+      return "pages must hold a multiple of 16 tokens, and pages and page table be sized within range";
+    case QM_ERR_ROTARY:
+      return "rotary columns must be a multiple of 16 up to d with a table that holds their "
+             "positions, eps finite and not negative, interleaved 0 or 1";
+    case QM_ERR_STRIDE: return "strides must be multiples of 8 elements and not negative";
+    case QM_ERR_WORKSPACE: return "the workspace is smaller than the call needs";
   }
   return "unknown status";
 }

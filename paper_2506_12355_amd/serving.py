@@ -1,0 +1,299 @@
+"""The operators around the attention forward that serve a model: head norms with the
+position rotation, a paged cache of keys and values, and attention of new tokens over it.
+
+As in ``binding``: argument marshalling only, on torch's memory and streams; every step
+runs in the gfx950 kernels of the library (``include/qm_attn.h``).
+
+The cache is two tensors of pages, [num_pages, Hkv, page_size, d] (``cache_layout``
+"bhnd") or [num_pages, page_size, Hkv, d] ("bnhd"), of the model's 16-bit type or
+``float8_e4m3fn`` (or ``uint8`` E4M3 codes), and a page table [B, columns] of int32: token
+t of sequence b is row t % page_size of page ``page_table[b, t // page_size]``.
+"""
+from __future__ import annotations
+
+import ctypes
+import functools
+
+from .binding import (QM_BHND, QM_BNHD, QM_OK, QmAttnError, _dtype_code, _enqueue, _int32,
+                      load_library, strerror)
+
+QM_E4M3 = 2   # qm_dtype_t: cached keys and values
+
+_LAYOUTS = {"bhnd": QM_BHND, "bnhd": QM_BNHD}
+_Strides = ctypes.c_longlong * 3
+
+
+def _layout_code(layout, name="layout"):
+    code = _LAYOUTS.get(layout)
+    if code is None:
+        raise ValueError(f"{name} must be 'bhnd' or 'bnhd', not {layout!r}")
+    return code
+
+
+def _on(device, name, t):
+    """The kernels follow device pointers: every tensor is on the queries' device."""
+    if t.device != device:
+        raise ValueError(f"{name} must be on the queries' device {device}, not {t.device}")
+
+
+def _queries(q):
+    """The device of q, which must be a ROCm tensor, and its type's code."""
+    if not q.is_cuda:
+        raise ValueError("q must be on a ROCm device")
+    return q.device, _dtype_code(q)
+
+
+def _rows(name, t, dtype, device, layout):
+    """Sizes (B, N, heads, d) of a [B, heads, N, d] or [B, N, heads, d] tensor whose
+    columns are contiguous, and its strides for the library (None: contiguous)."""
+    if t.dim() != 4:
+        raise ValueError(f"{name} must have shape {'[B, N, heads, d]' if layout else '[B, heads, N, d]'}")
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, not {t.dtype}")
+    _on(device, name, t)
+    size = t.shape
+    if layout:
+        size = (size[0], size[1], size[2], size[3])
+    else:
+        size = (size[0], size[2], size[1], size[3])
+    if t.is_contiguous():
+        return size, None
+    s = t.stride()
+    if s[3] != 1:
+        raise ValueError(f"{name}'s columns must be contiguous")
+    return size, _Strides(s[0], s[1], s[2]) if layout else _Strides(s[0], s[2], s[1])
+
+
+def _vector(name, t, size, device, dtype):
+    """The address of a contiguous tensor of `size`, or None for None."""
+    if t is None:
+        return None
+    if tuple(t.shape) != size or t.dtype != dtype or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {list(size)} tensor of {dtype}")
+    _on(device, name, t)
+    return t.data_ptr()
+
+
+def _output(name, out, like_shape, dtype, device):
+    import torch
+    if out is None:
+        return torch.empty(like_shape, dtype=dtype, device=device)
+    if tuple(out.shape) != tuple(like_shape) or out.dtype != dtype or not out.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {list(like_shape)} tensor of {dtype}")
+    _on(device, name, out)
+    return out
+
+
+def _angles(cos, sin, device):
+    """Addresses of the rotation's table, its rows and the columns it rotates."""
+    import torch
+    if cos is None and sin is None:
+        return None, None, 0, 0
+    if cos is None or sin is None:
+        raise ValueError("cos and sin are given together")
+    if cos.dim() != 2 or sin.shape != cos.shape:
+        raise ValueError("cos and sin must have shape [positions, rotary / 2]")
+    size = tuple(cos.shape)
+    return (_vector("cos", cos, size, device, torch.float32),
+            _vector("sin", sin, size, device, torch.float32), size[0], 2 * size[1])
+
+
+def _cache(k_cache, v_cache, page_table, B, Hkv, d, dtype, code, device, cache_layout):
+    """Cache arguments, checked: (num_pages, page_size, columns, cache type, layout)."""
+    import torch
+    layout = _layout_code(cache_layout, "cache_layout")
+    if k_cache.dim() != 4 or v_cache.shape != k_cache.shape:
+        raise ValueError("k_cache and v_cache must have one shape, "
+                         + ("[pages, page_size, Hkv, d]" if layout else "[pages, Hkv, page_size, d]"))
+    if v_cache.dtype != k_cache.dtype:
+        raise TypeError("k_cache and v_cache must have the same dtype")
+    if k_cache.dtype == dtype:
+        kind = code
+    elif k_cache.dtype in (torch.float8_e4m3fn, torch.uint8):
+        kind = QM_E4M3
+    else:
+        raise TypeError(f"the cache must be {dtype}, float8_e4m3fn or uint8, not {k_cache.dtype}")
+    for name, t in (("k_cache", k_cache), ("v_cache", v_cache)):
+        _on(device, name, t)
+        if not t.is_contiguous():
+            raise ValueError(f"{name} must be contiguous")
+    pages, a, b, width = k_cache.shape
+    heads, page_size = (b, a) if layout else (a, b)
+    if width != d or (Hkv is not None and heads != Hkv):
+        raise ValueError("the cache must hold the keys' heads and width")
+    if page_table.dim() != 2 or page_table.shape[0] != B:
+        raise ValueError("page_table must have shape [B, columns]")
+    _vector("page_table", page_table, tuple(page_table.shape), device, torch.int32)
+    return pages, page_size, heads, page_table.shape[1], kind, layout
+
+
+def qk_norm_rope(q, k, cos=None, sin=None, q_weight=None, k_weight=None, eps: float = 1e-6,
+                 starts=None, counts=None, interleaved: bool = False, q_out=None, k_out=None,
+                 stream=None, layout: str = "bhnd"):
+    """Norm of each query and key head and rotation by its token's position, in one pass.
+
+    q is [B, H, N, d] and k [B, Hkv, N, d] float16 or bfloat16 (``layout="bnhd"``:
+    [B, N, heads, d]), d 64 or 128.  Any strides that are multiples of 8 elements are
+    taken, so both may be views into one projection's output, or transposed ones, as
+    long as the d columns lie together.  Each row is divided by sqrt(mean(x^2) + eps) and
+    multiplied by ``q_weight`` or ``k_weight`` [d] (None: that tensor is not normalised),
+    then its first columns are rotated by the angles whose ``cos`` and ``sin`` [positions,
+    rotary / 2] (float32; None: no rotation) stand in the row of the token's position,
+    ``starts[b]`` (int32 [B]; None: 0) + t.  Pair j is columns (j, j + rotary / 2), or
+    (2 j, 2 j + 1) with ``interleaved``.  All in float32, rounded once.
+
+    ``counts`` (int32 [B]; None: N): rows of a padded batch past them are written as
+    zeros.  A position outside the table gives NaN rows.  Returns (q_out, k_out),
+    contiguous in ``layout``, as ``fwd`` and ``fwd_window`` take them
+    (``qm_qk_norm_rope``)."""
+    import torch
+    device, code = _queries(q)
+    lay = _layout_code(layout)
+    (B, N, H, d), qs = _rows("q", q, q.dtype, device, lay)
+    (Bk, Nk, Hkv, dk), ks = _rows("k", k, q.dtype, device, lay)
+    if Bk != B or Nk != N or dk != d:
+        raise ValueError("k must match q in B, N and d")
+    c, s, table_rows, rotary = _angles(cos, sin, device)
+    args = (_vector("q_weight", q_weight, (d,), device, q.dtype),
+            _vector("k_weight", k_weight, (d,), device, q.dtype), c, s,
+            _vector("starts", starts, (B,), device, torch.int32),
+            _vector("counts", counts, (B,), device, torch.int32),
+            B, H, Hkv, N, d, rotary, table_rows, float(eps), 1 if interleaved else 0, qs, ks)
+    q_out = _output("q_out", q_out, q.shape, q.dtype, device)
+    k_out = _output("k_out", k_out, k.shape, q.dtype, device)
+    _enqueue(load_library().qm_qk_norm_rope, device, stream,
+             (q.data_ptr(), k.data_ptr(), q_out.data_ptr(), k_out.data_ptr()) + args, (code, lay))
+    return q_out, k_out
+
+
+def qk_norm_rope_append(q, k, v, k_cache, v_cache, page_table, starts=None, cos=None, sin=None,
+                        q_weight=None, k_weight=None, eps: float = 1e-6, counts=None,
+                        interleaved: bool = False, k_scale: float = 1.0, v_scale: float = 1.0,
+                        q_out=None, k_out=None, stream=None, layout: str = "bhnd",
+                        cache_layout: str = "bhnd"):
+    """:func:`qk_norm_rope`, with the keys and the values v written to a paged cache:
+    token t of sequence b at position ``starts[b]`` + t, rows past ``counts`` not at all.
+
+    The cache holds key / ``k_scale`` and value / ``v_scale`` (with E4M3 pages, values
+    beyond 448 as 448).  Its pages past a sequence's tokens are left as they were, and so
+    are the entries of ``page_table`` that name them.  A token whose position has no page
+    (or no angle, or a page number out of range) is not stored.  v has k's shape and any
+    strides as q and k; ``k_out``, where given, receives the keys as ``qk_norm_rope``
+    returns them.  Without cos, sin and weights the keys are stored as they are.  Returns
+    q_out (``qm_qk_norm_rope_append``)."""
+    import torch
+    device, code = _queries(q)
+    lay = _layout_code(layout)
+    (B, N, H, d), qs = _rows("q", q, q.dtype, device, lay)
+    (Bk, Nk, Hkv, dk), ks = _rows("k", k, q.dtype, device, lay)
+    size_v, vs = _rows("v", v, q.dtype, device, lay)
+    if Bk != B or Nk != N or dk != d or size_v != (B, N, Hkv, d):
+        raise ValueError("k and v must have one shape and match q in B, N and d")
+    c, s, table_rows, rotary = _angles(cos, sin, device)
+    pages, page_size, _, columns, kind, cache_lay = _cache(
+        k_cache, v_cache, page_table, B, Hkv, d, q.dtype, code, device, cache_layout)
+    args = (k_cache.data_ptr(), v_cache.data_ptr(), page_table.data_ptr(),
+            _vector("q_weight", q_weight, (d,), device, q.dtype),
+            _vector("k_weight", k_weight, (d,), device, q.dtype), c, s,
+            _vector("starts", starts, (B,), device, torch.int32),
+            _vector("counts", counts, (B,), device, torch.int32),
+            B, H, Hkv, N, d, rotary, table_rows, float(eps), 1 if interleaved else 0,
+            pages, page_size, columns, float(k_scale), float(v_scale), qs, ks, vs)
+    q_out = _output("q_out", q_out, q.shape, q.dtype, device)
+    if k_out is not None:
+        k_out = _output("k_out", k_out, k.shape, q.dtype, device).data_ptr()
+    _enqueue(load_library().qm_qk_norm_rope_append, device, stream,
+             (q.data_ptr(), k.data_ptr(), v.data_ptr(), q_out.data_ptr(), k_out) + args,
+             (code, lay, kind, cache_lay))
+    return q_out
+
+
+@functools.lru_cache(maxsize=1024)
+def _workspace_bytes(index, *sizes) -> int:
+    """Workspace of a decode call of these sizes on device `index` (sizes alone decide)."""
+    import torch
+    need = ctypes.c_size_t()
+    with torch.cuda.device(index):
+        status = load_library().qm_attn_decode_workspace(*sizes, ctypes.byref(need))
+    if status != QM_OK:
+        raise QmAttnError(status, strerror(status))
+    return need.value
+
+
+def decode_workspace(q, k_cache, page_table, max_length: int | None = None,
+                     window: int | None = None, sinks: int = 0, cache_layout: str = "bhnd") -> int:
+    """Bytes of workspace that :func:`decode` needs for these arguments (0: none)."""
+    device, _ = _queries(q)
+    layout = _layout_code(cache_layout, "cache_layout")
+    B, H, d = q.shape
+    heads, page_size = (k_cache.shape[2], k_cache.shape[1]) if layout else k_cache.shape[1:3]
+    return _workspace_bytes(device.index, B, H, heads, d, page_size, page_table.shape[1],
+                            2 ** 31 - 1 if max_length is None else _int32(max_length, "max_length"),
+                            0 if window is None else _window(window), _int32(sinks, "sinks"))
+
+
+def _window(window) -> int:
+    window = _int32(window, "window")
+    if window < 1:
+        raise ValueError("window must be at least 1 (None: every cached token is visible)")
+    return window
+
+
+def decode(q, k_cache, v_cache, page_table, lengths, scale: float | None = None,
+           window: int | None = None, sinks: int = 0, k_scale: float = 1.0, v_scale: float = 1.0,
+           max_length: int | None = None, out=None, lse=None, workspace=None, stream=None,
+           cache_layout: str = "bhnd"):
+    """Attention of one new token per sequence over a paged cache.
+
+    q is [B, H, d] float16 or bfloat16, d 64 or 128; query head h reads key/value head
+    h // (H // Hkv) of the cache, whose real values are ``k_scale`` and ``v_scale`` times
+    what it holds.  ``lengths`` (int32 [B]) counts each sequence's cached tokens, the new
+    one's among them.  ``window``: only the last ``window`` of them and the first
+    ``sinks`` are visible, as for the last row of ``fwd_window``.
+
+    Returns (o [B, H, d], lse float32 [B, H]).  Length 0 gives o = 0 and lse = -inf; a
+    length below 0, above ``max_length`` or beyond the page table, or a page number out of
+    range, gives NaN for that sequence.  ``max_length`` is a bound that the host knows
+    (None: what the page table can hold); the work is split for it, so a close one is
+    faster.  ``workspace``: a uint8 tensor of :func:`decode_workspace` bytes (None: one is
+    allocated on the call's stream); two calls that may run at once need one each.
+    ``scale`` defaults to 1/sqrt(d) rounded to float32.  (``qm_attn_decode``)"""
+    import torch
+    device, code = _queries(q)
+    if q.dim() != 3 or not q.is_contiguous():
+        raise ValueError("q must be a contiguous [B, H, d] tensor")
+    B, H, d = q.shape
+    pages, page_size, Hkv, columns, kind, cache_lay = _cache(
+        k_cache, v_cache, page_table, B, None, d, q.dtype, code, device, cache_layout)
+    lens = _vector("lengths", lengths, (B,), device, torch.int32)
+    if lens is None:
+        raise ValueError("lengths must be given")
+    scale = 1.0 / d ** 0.5 if scale is None else float(scale)   # rounded to float32 by the call
+    window = 0 if window is None else _window(window)
+    sinks = _int32(sinks, "sinks")
+    most = 2 ** 31 - 1 if max_length is None else _int32(max_length, "max_length")
+    out = _output("out", out, (B, H, d), q.dtype, device)
+    lse = _output("lse", lse, (B, H), torch.float32, device)
+    need = _workspace_bytes(device.index, B, H, Hkv, d, page_size, columns, most, window, sinks)
+    if workspace is not None:
+        if workspace.dtype != torch.uint8 or workspace.dim() != 1 or not workspace.is_contiguous():
+            raise ValueError("workspace must be a contiguous 1-D uint8 tensor")
+        _on(device, "workspace", workspace)
+        ws, given = workspace.data_ptr(), workspace.numel()
+    elif need:
+        # from the pool of the stream that will use it: freed on return, its memory is
+        # given out again in that stream's order only
+        if stream is None:
+            workspace = torch.empty(need, dtype=torch.uint8, device=device)
+        else:
+            with torch.cuda.stream(stream):
+                workspace = torch.empty(need, dtype=torch.uint8, device=device)
+        ws, given = workspace.data_ptr(), need
+    else:
+        ws, given = None, 0
+    _enqueue(load_library().qm_attn_decode, device, stream,
+             (q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), out.data_ptr(), lse.data_ptr(),
+              page_table.data_ptr(), lens, B, H, Hkv, d, pages, page_size, columns, most, scale,
+              float(k_scale), float(v_scale), window, sinks, ws, given),
+             (code, kind, cache_lay))
+    return out, lse
