@@ -195,18 +195,20 @@ int plan(int B, int H, int Hkv, int d, int page_size, int table_cols, int max_le
   *limit = (int)(max_length < capacity ? max_length : capacity);
   const uint64_t tiles = ((uint64_t)(H / Hkv) + 15) / 16;
   const uint64_t rows = times(times((uint64_t)B, (uint64_t)Hkv), tiles);
-  if (rows > INT_MAX / 256 || times((uint64_t)B, (uint64_t)H) > INT_MAX / 64) return QM_ERR_SHAPE;
+  if (rows > INT_MAX / 512 || times((uint64_t)B, (uint64_t)H) > INT_MAX / 256) return QM_ERR_SHAPE;
   int id = 0, cus = 0;
   if (hipGetDevice(&id) != hipSuccess ||
       hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, id) != hipSuccess)
     return QM_ERR_LAUNCH;
   *p = qm::plan_decode((int64_t)rows, qm::decode_blocks(*limit, window, sinks), cus);
-  if (rows * (uint64_t)p->splits > INT_MAX / 256) return QM_ERR_SHAPE;
   return QM_OK;
 }
 
-size_t workspace_of(const qm::DecodePlan& p, int B, int H, int d) {
-  return p.splits > 1 ? (size_t)B * H * p.splits * (d + 2) * sizeof(float) : 0;
+// Two partial results of 16 heads for each workgroup of a call in shares, and two
+// numbers for each row.
+size_t workspace_of(const qm::DecodePlan& p, int B, int H, int Hkv, int d) {
+  const size_t rows = (size_t)B * Hkv * ((H / Hkv + 15) / 16);
+  return p.grid ? (size_t)2 * p.grid * 16 * (d + 2) * sizeof(float) + rows * 2 * sizeof(int32_t) : 0;
 }
 
 }  // namespace
@@ -243,7 +245,7 @@ extern "C" int qm_attn_decode_workspace(int B, int H, int Hkv, int d, int page_s
   qm::DecodePlan p;
   int limit;
   const int st = plan(B, H, Hkv, d, page_size, table_cols, max_length, window, sinks, &p, &limit);
-  if (st == QM_OK) *bytes = workspace_of(p, B, H, d);
+  if (st == QM_OK) *bytes = workspace_of(p, B, H, Hkv, d);
   return st;
 }
 
@@ -269,7 +271,7 @@ extern "C" int qm_attn_decode(const void* q, const void* k_cache, const void* v_
       !(fabs(c) < (double)FLT_MAX))
     return QM_ERR_SCALE;
   const uint64_t rows = times((uint64_t)B, (uint64_t)H);
-  if (rows > INT_MAX / 64) return QM_ERR_SHAPE;
+  if (rows > INT_MAX / 256) return QM_ERR_SHAPE;
   const Range in[] = {{q, rows * d * 2}, {k_cache, cache_bytes}, {v_cache, cache_bytes},
                       {page_table, (uint64_t)B * (uint64_t)table_cols * 4}, {lengths, (uint64_t)B * 4}};
   const Range ro = {o, rows * d * 2}, rl = {lse, rows * 4};
@@ -281,7 +283,7 @@ extern "C" int qm_attn_decode(const void* q, const void* k_cache, const void* v_
   qm::DecodePlan p;
   st = plan(B, H, Hkv, d, page_size, table_cols, max_length, window, sinks, &p, &a.limit);
   if (st != QM_OK) return st;
-  const size_t need = workspace_of(p, B, H, d);
+  const size_t need = workspace_of(p, B, H, Hkv, d);
   if (need) {
     if (!workspace || workspace_bytes < need) return QM_ERR_WORKSPACE;
     const Range rw = {workspace, need};

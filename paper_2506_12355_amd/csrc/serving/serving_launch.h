@@ -47,10 +47,10 @@ struct DecodeArgs {
   float* workspace;
 };
 
-// How a decode call splits the cached tokens: workgroups of `waves` wavefronts take
-// `chunk` 32-token blocks of a sequence's visible ones, at most `splits` per sequence.
+// How a decode call is divided: a workgroup for each row (grid 0), or equal shares of
+// all rows' blocks for `grid` workgroups, then joined.
 struct DecodePlan {
-  int waves, chunk, splits;
+  int grid;
 };
 
 hipError_t launch_decode(const DecodeArgs& a, const DecodePlan& plan, hipStream_t stream);
