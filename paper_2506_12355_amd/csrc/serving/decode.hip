@@ -184,14 +184,15 @@ __device__ __forceinline__ void piece(const Params& p, float* lds, int b, int ro
   const uint32_t v_lane = 4 * g * p.token_stride + n * (CV * ES);
 
   // Offsets of the tiles of the wavefront's next 32 blocks: lane 2 i + t holds tile t of
-  // the i-th.  A tile past the length borrows the first tile's (its keys are hidden).
+  // the i-th.  A tile without a visible key may have no page: it borrows its neighbour's
+  // (a block on the list has a visible key in one of the two), and its keys are hidden.
   int off_lo = 0, off_hi = 0;
   auto look_up = [&](int i0) __attribute__((always_inline)) {
     const int li = i0 + WAVES * (lane >> 1);
     int64_t off = 0;
     if (li < hi) {
       int token = blocks.token(li) + 16 * (lane & 1);
-      if (token >= len) token -= 16;
+      if (token >= len || (token + 16 <= lo_window && token >= p.sinks)) token ^= 16;
       const uint32_t at = p.page.div((uint32_t)token);
       const int page = p.table[(size_t)b * p.table_cols + at];
       if (page >= 0 && page < p.num_pages)

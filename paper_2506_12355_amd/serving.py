@@ -21,7 +21,12 @@ QM_E4M3 = 2   # qm_dtype_t: cached keys and values
 
 _LAYOUTS = {"bhnd": QM_BHND, "bnhd": QM_BNHD}
 _Strides = ctypes.c_longlong * 3
+_MOST = 2 ** 31 - 1   # no bound on lengths but the page table's
 
+
+# The checks below read each property of a tensor once and put off what a message needs
+# until there is one: a call of one token takes the GPU a few microseconds, and its
+# arguments took the host 11 (now 6; allocating the outputs and the launch come on top).
 
 def _layout_code(layout, name="layout"):
     code = _LAYOUTS.get(layout)
@@ -30,32 +35,33 @@ def _layout_code(layout, name="layout"):
     return code
 
 
-def _on(device, name, t):
-    """The kernels follow device pointers: every tensor is on the queries' device."""
-    if t.device != device:
-        raise ValueError(f"{name} must be on the queries' device {device}, not {t.device}")
-
-
 def _queries(q):
-    """The device of q, which must be a ROCm tensor, and its type's code."""
+    """The device index of q, which must be a ROCm tensor, and its type and the type's code."""
     if not q.is_cuda:
         raise ValueError("q must be on a ROCm device")
-    return q.device, _dtype_code(q)
+    return q.get_device(), q.dtype, _dtype_code(q)
 
 
-def _rows(name, t, dtype, device, layout):
+def _elsewhere(name, t, index):
+    """The kernels follow device pointers: every tensor is on the queries' device."""
+    return ValueError(f"{name} must be on the queries' device cuda:{index}, not {t.device}")
+
+
+def _rows(name, t, dtype, index, layout):
     """Sizes (B, N, heads, d) of a [B, heads, N, d] or [B, N, heads, d] tensor whose
     columns are contiguous, and its strides for the library (None: contiguous)."""
-    if t.dim() != 4:
-        raise ValueError(f"{name} must have shape {'[B, N, heads, d]' if layout else '[B, heads, N, d]'}")
-    if t.dtype != dtype:
-        raise TypeError(f"{name} must be {dtype}, not {t.dtype}")
-    _on(device, name, t)
     size = t.shape
+    if len(size) != 4:
+        raise ValueError(f"{name} must have shape {'[B, N, heads, d]' if layout else '[B, heads, N, d]'}")
+    if t.dtype is not dtype:
+        raise TypeError(f"{name} must be {dtype}, not {t.dtype}")
+    if t.get_device() != index:
+        raise _elsewhere(name, t, index)
     if layout:
-        size = (size[0], size[1], size[2], size[3])
+        size = tuple(size)
     else:
-        size = (size[0], size[2], size[1], size[3])
+        B, heads, N, d = size
+        size = (B, N, heads, d)
     if t.is_contiguous():
         return size, None
     s = t.stride()
@@ -64,67 +70,79 @@ def _rows(name, t, dtype, device, layout):
     return size, _Strides(s[0], s[1], s[2]) if layout else _Strides(s[0], s[2], s[1])
 
 
-def _vector(name, t, size, device, dtype):
+def _vector(name, t, size, index, dtype):
     """The address of a contiguous tensor of `size`, or None for None."""
     if t is None:
         return None
-    if tuple(t.shape) != size or t.dtype != dtype or not t.is_contiguous():
+    if t.shape != size or t.dtype is not dtype or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous {list(size)} tensor of {dtype}")
-    _on(device, name, t)
+    if t.get_device() != index:
+        raise _elsewhere(name, t, index)
     return t.data_ptr()
 
 
-def _output(name, out, like_shape, dtype, device):
-    import torch
+def _output(name, out, like, index):
+    """The caller's output, checked, or a new contiguous tensor shaped like `like`."""
     if out is None:
-        return torch.empty(like_shape, dtype=dtype, device=device)
-    if tuple(out.shape) != tuple(like_shape) or out.dtype != dtype or not out.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous {list(like_shape)} tensor of {dtype}")
-    _on(device, name, out)
+        if type(like) is _torch().Tensor and like.is_contiguous():
+            return _torch().empty_like(like)
+        return _torch().empty(like.shape, dtype=like.dtype, device=like.device)
+    _vector(name, out, like.shape, index, like.dtype)
     return out
 
 
-def _angles(cos, sin, device):
+def _angles(cos, sin, index):
     """Addresses of the rotation's table, its rows and the columns it rotates."""
-    import torch
     if cos is None and sin is None:
         return None, None, 0, 0
     if cos is None or sin is None:
         raise ValueError("cos and sin are given together")
-    if cos.dim() != 2 or sin.shape != cos.shape:
+    size = cos.shape
+    if len(size) != 2 or sin.shape != size:
         raise ValueError("cos and sin must have shape [positions, rotary / 2]")
-    size = tuple(cos.shape)
-    return (_vector("cos", cos, size, device, torch.float32),
-            _vector("sin", sin, size, device, torch.float32), size[0], 2 * size[1])
+    f32 = _torch().float32
+    return (_vector("cos", cos, size, index, f32), _vector("sin", sin, size, index, f32),
+            2 * size[1], size[0])
 
 
-def _cache(k_cache, v_cache, page_table, B, Hkv, d, dtype, code, device, cache_layout):
-    """Cache arguments, checked: (num_pages, page_size, columns, cache type, layout)."""
+@functools.lru_cache(maxsize=1)
+def _torch():
     import torch
+    return torch
+
+
+@functools.lru_cache(maxsize=64)
+def _device(index):
+    return _torch().device("cuda", index)
+
+
+def _cache(k_cache, v_cache, page_table, B, d, dtype, code, index, cache_layout):
+    """Cache arguments, checked: (num_pages, page_size, heads, columns, cache type, layout)."""
     layout = _layout_code(cache_layout, "cache_layout")
-    if k_cache.dim() != 4 or v_cache.shape != k_cache.shape:
+    size, kind = k_cache.shape, k_cache.dtype
+    if len(size) != 4 or v_cache.shape != size:
         raise ValueError("k_cache and v_cache must have one shape, "
                          + ("[pages, page_size, Hkv, d]" if layout else "[pages, Hkv, page_size, d]"))
-    if v_cache.dtype != k_cache.dtype:
+    if v_cache.dtype is not kind:
         raise TypeError("k_cache and v_cache must have the same dtype")
-    if k_cache.dtype == dtype:
-        kind = code
-    elif k_cache.dtype in (torch.float8_e4m3fn, torch.uint8):
-        kind = QM_E4M3
-    else:
-        raise TypeError(f"the cache must be {dtype}, float8_e4m3fn or uint8, not {k_cache.dtype}")
-    for name, t in (("k_cache", k_cache), ("v_cache", v_cache)):
-        _on(device, name, t)
-        if not t.is_contiguous():
-            raise ValueError(f"{name} must be contiguous")
-    pages, a, b, width = k_cache.shape
-    heads, page_size = (b, a) if layout else (a, b)
-    if width != d or (Hkv is not None and heads != Hkv):
-        raise ValueError("the cache must hold the keys' heads and width")
-    if page_table.dim() != 2 or page_table.shape[0] != B:
+    if kind is not dtype:
+        if kind not in (_torch().float8_e4m3fn, _torch().uint8):
+            raise TypeError(f"the cache must be {dtype}, float8_e4m3fn or uint8, not {kind}")
+        code = QM_E4M3
+    if not (k_cache.is_contiguous() and v_cache.is_contiguous()):
+        raise ValueError("k_cache and v_cache must be contiguous")
+    if k_cache.get_device() != index or v_cache.get_device() != index:
+        raise _elsewhere("the cache", v_cache if k_cache.get_device() == index else k_cache, index)
+    pages, heads, page_size, width = size
+    if layout:
+        heads, page_size = page_size, heads
+    if width != d:
+        raise ValueError("the cache must have the queries' width")
+    table = page_table.shape
+    if len(table) != 2 or table[0] != B:
         raise ValueError("page_table must have shape [B, columns]")
-    _vector("page_table", page_table, tuple(page_table.shape), device, torch.int32)
-    return pages, page_size, heads, page_table.shape[1], kind, layout
+    _vector("page_table", page_table, table, index, _torch().int32)
+    return pages, page_size, heads, table[1], code, layout
 
 
 def qk_norm_rope(q, k, cos=None, sin=None, q_weight=None, k_weight=None, eps: float = 1e-6,
@@ -146,22 +164,22 @@ def qk_norm_rope(q, k, cos=None, sin=None, q_weight=None, k_weight=None, eps: fl
     zeros.  A position outside the table gives NaN rows.  Returns (q_out, k_out),
     contiguous in ``layout``, as ``fwd`` and ``fwd_window`` take them
     (``qm_qk_norm_rope``)."""
-    import torch
-    device, code = _queries(q)
+    index, dtype, code = _queries(q)
     lay = _layout_code(layout)
-    (B, N, H, d), qs = _rows("q", q, q.dtype, device, lay)
-    (Bk, Nk, Hkv, dk), ks = _rows("k", k, q.dtype, device, lay)
+    (B, N, H, d), qs = _rows("q", q, dtype, index, lay)
+    (Bk, Nk, Hkv, dk), ks = _rows("k", k, dtype, index, lay)
     if Bk != B or Nk != N or dk != d:
         raise ValueError("k must match q in B, N and d")
-    c, s, table_rows, rotary = _angles(cos, sin, device)
-    args = (_vector("q_weight", q_weight, (d,), device, q.dtype),
-            _vector("k_weight", k_weight, (d,), device, q.dtype), c, s,
-            _vector("starts", starts, (B,), device, torch.int32),
-            _vector("counts", counts, (B,), device, torch.int32),
+    c, s, rotary, table_rows = _angles(cos, sin, index)
+    i32, sequences, columns = _torch().int32, (B,), (d,)
+    args = (_vector("q_weight", q_weight, columns, index, dtype),
+            _vector("k_weight", k_weight, columns, index, dtype), c, s,
+            _vector("starts", starts, sequences, index, i32),
+            _vector("counts", counts, sequences, index, i32),
             B, H, Hkv, N, d, rotary, table_rows, float(eps), 1 if interleaved else 0, qs, ks)
-    q_out = _output("q_out", q_out, q.shape, q.dtype, device)
-    k_out = _output("k_out", k_out, k.shape, q.dtype, device)
-    _enqueue(load_library().qm_qk_norm_rope, device, stream,
+    q_out = _output("q_out", q_out, q, index)
+    k_out = _output("k_out", k_out, k, index)
+    _enqueue(load_library().qm_qk_norm_rope, _device(index), stream,
              (q.data_ptr(), k.data_ptr(), q_out.data_ptr(), k_out.data_ptr()) + args, (code, lay))
     return q_out, k_out
 
@@ -181,28 +199,30 @@ def qk_norm_rope_append(q, k, v, k_cache, v_cache, page_table, starts=None, cos=
     strides as q and k; ``k_out``, where given, receives the keys as ``qk_norm_rope``
     returns them.  Without cos, sin and weights the keys are stored as they are.  Returns
     q_out (``qm_qk_norm_rope_append``)."""
-    import torch
-    device, code = _queries(q)
+    index, dtype, code = _queries(q)
     lay = _layout_code(layout)
-    (B, N, H, d), qs = _rows("q", q, q.dtype, device, lay)
-    (Bk, Nk, Hkv, dk), ks = _rows("k", k, q.dtype, device, lay)
-    size_v, vs = _rows("v", v, q.dtype, device, lay)
+    (B, N, H, d), qs = _rows("q", q, dtype, index, lay)
+    (Bk, Nk, Hkv, dk), ks = _rows("k", k, dtype, index, lay)
+    size_v, vs = _rows("v", v, dtype, index, lay)
     if Bk != B or Nk != N or dk != d or size_v != (B, N, Hkv, d):
         raise ValueError("k and v must have one shape and match q in B, N and d")
-    c, s, table_rows, rotary = _angles(cos, sin, device)
-    pages, page_size, _, columns, kind, cache_lay = _cache(
-        k_cache, v_cache, page_table, B, Hkv, d, q.dtype, code, device, cache_layout)
+    c, s, rotary, table_rows = _angles(cos, sin, index)
+    pages, page_size, heads, table_columns, kind, cache_lay = _cache(
+        k_cache, v_cache, page_table, B, d, dtype, code, index, cache_layout)
+    if heads != Hkv:
+        raise ValueError("the cache must have the keys' heads")
+    i32, sequences, columns = _torch().int32, (B,), (d,)
     args = (k_cache.data_ptr(), v_cache.data_ptr(), page_table.data_ptr(),
-            _vector("q_weight", q_weight, (d,), device, q.dtype),
-            _vector("k_weight", k_weight, (d,), device, q.dtype), c, s,
-            _vector("starts", starts, (B,), device, torch.int32),
-            _vector("counts", counts, (B,), device, torch.int32),
+            _vector("q_weight", q_weight, columns, index, dtype),
+            _vector("k_weight", k_weight, columns, index, dtype), c, s,
+            _vector("starts", starts, sequences, index, i32),
+            _vector("counts", counts, sequences, index, i32),
             B, H, Hkv, N, d, rotary, table_rows, float(eps), 1 if interleaved else 0,
-            pages, page_size, columns, float(k_scale), float(v_scale), qs, ks, vs)
-    q_out = _output("q_out", q_out, q.shape, q.dtype, device)
+            pages, page_size, table_columns, float(k_scale), float(v_scale), qs, ks, vs)
+    q_out = _output("q_out", q_out, q, index)
     if k_out is not None:
-        k_out = _output("k_out", k_out, k.shape, q.dtype, device).data_ptr()
-    _enqueue(load_library().qm_qk_norm_rope_append, device, stream,
+        k_out = _output("k_out", k_out, k, index).data_ptr()
+    _enqueue(load_library().qm_qk_norm_rope_append, _device(index), stream,
              (q.data_ptr(), k.data_ptr(), v.data_ptr(), q_out.data_ptr(), k_out) + args,
              (code, lay, kind, cache_lay))
     return q_out
@@ -223,12 +243,14 @@ def _workspace_bytes(index, *sizes) -> int:
 def decode_workspace(q, k_cache, page_table, max_length: int | None = None,
                      window: int | None = None, sinks: int = 0, cache_layout: str = "bhnd") -> int:
     """Bytes of workspace that :func:`decode` needs for these arguments (0: none)."""
-    device, _ = _queries(q)
-    layout = _layout_code(cache_layout, "cache_layout")
+    index, dtype, code = _queries(q)
+    if q.dim() != 3:
+        raise ValueError("q must have shape [B, H, d]")
     B, H, d = q.shape
-    heads, page_size = (k_cache.shape[2], k_cache.shape[1]) if layout else k_cache.shape[1:3]
-    return _workspace_bytes(device.index, B, H, heads, d, page_size, page_table.shape[1],
-                            2 ** 31 - 1 if max_length is None else _int32(max_length, "max_length"),
+    _, page_size, heads, columns, _, _ = _cache(k_cache, k_cache, page_table, B, d, dtype, code,
+                                                index, cache_layout)
+    return _workspace_bytes(index, B, H, heads, d, page_size, columns,
+                            _MOST if max_length is None else _int32(max_length, "max_length"),
                             0 if window is None else _window(window), _int32(sinks, "sinks"))
 
 
@@ -258,40 +280,44 @@ def decode(q, k_cache, v_cache, page_table, lengths, scale: float | None = None,
     faster.  ``workspace``: a uint8 tensor of :func:`decode_workspace` bytes (None: one is
     allocated on the call's stream); two calls that may run at once need one each.
     ``scale`` defaults to 1/sqrt(d) rounded to float32.  (``qm_attn_decode``)"""
-    import torch
-    device, code = _queries(q)
+    index, dtype, code = _queries(q)
     if q.dim() != 3 or not q.is_contiguous():
         raise ValueError("q must be a contiguous [B, H, d] tensor")
     B, H, d = q.shape
     pages, page_size, Hkv, columns, kind, cache_lay = _cache(
-        k_cache, v_cache, page_table, B, None, d, q.dtype, code, device, cache_layout)
-    lens = _vector("lengths", lengths, (B,), device, torch.int32)
-    if lens is None:
+        k_cache, v_cache, page_table, B, d, dtype, code, index, cache_layout)
+    torch = _torch()
+    if lengths is None:
         raise ValueError("lengths must be given")
+    lens = _vector("lengths", lengths, (B,), index, torch.int32)
     scale = 1.0 / d ** 0.5 if scale is None else float(scale)   # rounded to float32 by the call
     window = 0 if window is None else _window(window)
     sinks = _int32(sinks, "sinks")
-    most = 2 ** 31 - 1 if max_length is None else _int32(max_length, "max_length")
-    out = _output("out", out, (B, H, d), q.dtype, device)
-    lse = _output("lse", lse, (B, H), torch.float32, device)
-    need = _workspace_bytes(device.index, B, H, Hkv, d, page_size, columns, most, window, sinks)
+    most = _MOST if max_length is None else _int32(max_length, "max_length")
+    out = _output("out", out, q, index)
+    if lse is None:
+        lse = torch.empty(B, H, dtype=torch.float32, device=_device(index))
+    else:
+        _vector("lse", lse, (B, H), index, torch.float32)
+    need = _workspace_bytes(index, B, H, Hkv, d, page_size, columns, most, window, sinks)
     if workspace is not None:
-        if workspace.dtype != torch.uint8 or workspace.dim() != 1 or not workspace.is_contiguous():
+        if workspace.dtype is not torch.uint8 or workspace.dim() != 1 or not workspace.is_contiguous():
             raise ValueError("workspace must be a contiguous 1-D uint8 tensor")
-        _on(device, "workspace", workspace)
+        if workspace.get_device() != index:
+            raise _elsewhere("workspace", workspace, index)
         ws, given = workspace.data_ptr(), workspace.numel()
     elif need:
         # from the pool of the stream that will use it: freed on return, its memory is
         # given out again in that stream's order only
         if stream is None:
-            workspace = torch.empty(need, dtype=torch.uint8, device=device)
+            workspace = torch.empty(need, dtype=torch.uint8, device=_device(index))
         else:
             with torch.cuda.stream(stream):
-                workspace = torch.empty(need, dtype=torch.uint8, device=device)
+                workspace = torch.empty(need, dtype=torch.uint8, device=_device(index))
         ws, given = workspace.data_ptr(), need
     else:
         ws, given = None, 0
-    _enqueue(load_library().qm_attn_decode, device, stream,
+    _enqueue(load_library().qm_attn_decode, _device(index), stream,
              (q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), out.data_ptr(), lse.data_ptr(),
               page_table.data_ptr(), lens, B, H, Hkv, d, pages, page_size, columns, most, scale,
               float(k_scale), float(v_scale), window, sinks, ws, given),
