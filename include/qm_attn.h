@@ -287,6 +287,8 @@ int qm_attn_fwd_window(const void* q, const void* k, const void* v, void* o, flo
  * dimensions) split the keys between the wavefronts of 64- or 128-row
  * workgroups, whatever this setting is: into four groups from N = 384 on
  * (d = 64 and FP8), into two from N = 768 (d = 64) or 1536 (d = 128 and FP8).
+ * qm_attn_fwd_window has rules of its own for the same choices, with 128-row
+ * workgroups always at d = 64.
  *
  * Results do not depend on the setting: every query row takes the same
  * arithmetic in the same order under each, so outputs are byte-identical;

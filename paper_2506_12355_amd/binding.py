@@ -261,7 +261,7 @@ def _lse(q, lse, B, H, N):
     """The log-sum-exp output: the caller's, checked, or a new tensor."""
     import torch
     if lse is None:
-        return torch.empty((B, H, N), dtype=torch.float32, device=q.device)
+        return torch.empty(B, H, N, dtype=torch.float32, device=q.device)
     if lse.shape != (B, H, N) or lse.dtype != torch.float32 or not lse.is_contiguous():
         raise ValueError("lse must be a contiguous float32 tensor of shape [B, H, N]")
     return lse
@@ -313,8 +313,7 @@ def _checked(q, k, v, scale, out, lse, layout):
         raise ValueError("k must match q in B, N and d")
     if not (q.is_cuda and k.is_cuda and v.is_cuda):
         raise ValueError("q, k and v must be on a ROCm device")
-    device = q.device
-    if not (device == k.device == v.device):
+    if not (q.get_device() == k.get_device() == v.get_device()):
         raise ValueError("q, k and v must be on the same device")
     if not (q.dtype == k.dtype == v.dtype):
         raise TypeError("q, k and v must have the same dtype")
@@ -325,13 +324,17 @@ def _checked(q, k, v, scale, out, lse, layout):
     # the C float argument rounds the scale to float32
     scale = 1.0 / d ** 0.5 if scale is None else float(scale)
     if out is None:
-        out = torch.empty((*qs[:3], dv), dtype=q.dtype, device=device)
+        # (empty_like is a microsecond shorter, but would keep a subclass)
+        if dv == d and type(q) is torch.Tensor:
+            out = torch.empty_like(q)
+        else:
+            out = torch.empty((*qs[:3], dv), dtype=q.dtype, device=q.device)
     else:
         oshape = (*qs[:3], dv)
         if tuple(out.shape) != oshape or out.dtype != q.dtype or not out.is_contiguous():
             raise ValueError(f"out must be a contiguous {list(oshape)} tensor of q's dtype")
     lse = _lse(q, lse, B, H, N)
-    _check_outputs_on(device, out, lse)
+    _check_outputs_on(q.device, out, lse)
     args = (q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), lse.data_ptr(), B, H)
     return args, Hkv, N, d, dv, scale, code, out, lse
 

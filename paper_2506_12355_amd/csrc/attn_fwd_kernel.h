@@ -443,7 +443,7 @@ __device__ __forceinline__ void attn_fwd_body(const KParams& p) {
   constexpr int NMT = DV / 32;           // GEMM-II M tiles
   constexpr int BM = 32 * WAVES;         // query rows per workgroup
   static_assert(LV::NG % WAVES == 0, "each wave issues whole load groups");
-  static_assert(!WINDOW || (CAUSAL && G == 1), "windows are causal, without key groups");
+  static_assert(!WINDOW || (CAUSAL && !FP8), "windows are causal, of 16-bit types");
   constexpr int GPWV = LV::NG / WAVES;   // V direct loads per wave per block
   constexpr int RING = ring_depth<DK, DV, DT, WAVES, G>();
   // Deferred GEMM-II: with four-block rings, GEMM-II of block j can run in
@@ -519,8 +519,9 @@ __device__ __forceinline__ void attn_fwd_body(const KParams& p) {
   int nsink = 0, skip = 0;   // WINDOW: blocks of first keys, and blocks left out after them
   // the key block of this wave's group in step j
   auto key_block = [&](int j) {
-    if constexpr (WINDOW) return j < nsink ? j : j + skip;
-    else return G > 1 ? j * G + kgrp : j;
+    const int i = G > 1 ? j * G + kgrp : j;
+    if constexpr (WINDOW) return i < nsink ? i : i + skip;
+    else return i;
   };
 
   // ---- HBM -> LDS: this wave's load groups of one K or V block ----
@@ -592,7 +593,7 @@ __device__ __forceinline__ void attn_fwd_body(const KParams& p) {
       const int first = max(0, qb * BM - p.window + 1) / kBN;   // the block of the first row's window
       nsink = min(first, (p.sinks + kBN - 1) / kBN);
       skip = first - nsink;
-      nkv = nblk - skip;
+      nkv = (nblk - skip + G - 1) / G;
     }
     // lane: query row, k-group (OP::KGB bytes of each k-step)
     const uint32_t q_off = (uint32_t)(qb * BM + wave * 32 + (lane & 31)) * rs_q +
@@ -806,7 +807,9 @@ __device__ __forceinline__ void attn_fwd_body(const KParams& p) {
                      f32x16 (&s_next)[2], const Frag (&pin)[NPB], Frag (&pout)[NPB])
         __attribute__((always_inline)) {
       constexpr bool DEF = DEFER && !decltype(first)::value;   // GEMM-II of block j-1 here
-      using LoopWait = typename std::conditional<decltype(first)::value, Wait5, Wait1>::type;
+      // (a window's groups reload spilled descriptor words inside the loop too)
+      using LoopWait =
+          typename std::conditional<decltype(first)::value || (WINDOW && G > 1), Wait5, Wait1>::type;
       const int j0 = key_block(j) * kBN;
       constexpr int AHEAD = FP8 ? 2 : 4;              // operand reads ahead of their MFMA
       constexpr int NG1 = 2 * NKS;                    // GEMM-I MFMAs per block
@@ -827,17 +830,24 @@ __device__ __forceinline__ void attn_fwd_body(const KParams& p) {
 
       // mask: keys past the end of the sequence, keys after the query (causal)
       bool need_mask = (j0 + kBN > N) || (CAUSAL && j0 + kBN - 1 > qw);
-      // some key lies before some row's window and is no first key
-      if constexpr (WINDOW) need_mask |= j0 <= qw + 31 - p.window && j0 + kBN > p.sinks;
+      // some key lies before some row's window and is no first key (no mask for the end:
+      // a row of the sequence sees no key past its own)
+      if constexpr (WINDOW)
+        need_mask = j0 + kBN - 1 > qw || (j0 <= qw + 31 - p.window && j0 + kBN > p.sinks);
       if (need_mask) {
   #pragma unroll
         for (int kt = 0; kt < 2; ++kt) {
   #pragma unroll
           for (int r = 0; r < 16; ++r) {
             const int key = j0 + 32 * kt + 8 * (r / 4) + 4 * hi + (r % 4);
-            bool hidden = key >= N || (CAUSAL && key > qrow);
-            if constexpr (WINDOW) hidden |= key <= qrow - p.window && key >= p.sinks;
-            if (hidden) s[kt][r] = -INFINITY;
+            if constexpr (WINDOW) {
+              // in the window iff 0 <= qrow - key < window: one unsigned compare
+              bool hidden = (uint32_t)(qrow - key) >= (uint32_t)p.window;
+              if (j0 < p.sinks) hidden &= key >= p.sinks || key > qrow;
+              if (hidden) s[kt][r] = -INFINITY;
+            } else {
+              if (key >= N || (CAUSAL && key > qrow)) s[kt][r] = -INFINITY;
+            }
           }
         }
       }
@@ -1019,9 +1029,10 @@ __device__ __forceinline__ void attn_fwd_body(const KParams& p) {
     // Blocks this wave computes: 0 .. j_act-1 (causal: the blocks up to its
     // last row; none for a wave past the sequence end).  It still issues the
     // loads of the blocks after those, and takes every barrier.
-    const int b_act = (qw >= N) ? 0 : (CAUSAL ? min(nblk, (qw + 31) / kBN + 1) : nblk);
+    const int b_act =
+        (qw >= N) ? 0 : (CAUSAL ? min(nblk, (qw + 31) / kBN + 1) : nblk) - (WINDOW ? skip : 0);
     const int j_act =
-        WINDOW ? max(b_act - skip, 0) : G > 1 ? __builtin_amdgcn_readfirstlane((unsigned)(b_act - kgrp + G - 1) / G) : b_act;
+        G > 1 ? __builtin_amdgcn_readfirstlane((unsigned)(b_act - kgrp + G - 1) / G) : b_act;
     // The computed blocks run in one loop and the skipped ones in a second,
     // so that no block tests whether it computes; only the four-wave causal
     // d = 64 instance, at its register ceiling, keeps that test inside one
@@ -1176,8 +1187,8 @@ __device__ __forceinline__ void attn_fwd_body(const KParams& p) {
       // g OWN .. (g + 1) OWN - 1, so each wave gives the quads the others
       // finish to LDS (the rings' bytes, free now) and reads its own from
       // them.  A group that saw no visible key of a row holds m = -FLT_MAX,
-      // l = O = 0 there and gets weight 0: group 0 holds block 0, whose first
-      // key every row sees.
+      // l = O = 0 there and gets weight 0: some group holds a key that the row
+      // sees (block 0's first, or with a window the row's own).
       static_assert(OWN % 2 == 0, "each group finishes whole pairs of quads");
       auto slot_of = [](int src, int dst, int i) {   // 1 KB slot of quad i that src gives to dst
         return (src * (G - 1) + (dst < src ? dst : dst - 1)) * OWN + i;
