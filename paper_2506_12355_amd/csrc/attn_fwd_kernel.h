@@ -829,23 +829,46 @@ __device__ __forceinline__ void attn_fwd_body(const KParams& p) {
       }
 
       // mask: keys past the end of the sequence, keys after the query (causal)
-      bool need_mask = (j0 + kBN > N) || (CAUSAL && j0 + kBN - 1 > qw);
-      // some key lies before some row's window and is no first key (no mask for the end:
-      // a row of the sequence sees no key past its own)
-      if constexpr (WINDOW)
-        need_mask = j0 + kBN - 1 > qw || (j0 <= qw + 31 - p.window && j0 + kBN > p.sinks);
-      if (need_mask) {
+      if constexpr (WINDOW) {
+        // by halves of 32 keys: a wavefront's rows cross the diagonal in one of them, and
+        // the left edges of their windows in one or two.  Key off of a half is hidden iff
+        // off > d0 (past the row) or off <= d0 - window (before its window, and no first
+        // key); no mask for the end, as a row sees no key past its own.
   #pragma unroll
         for (int kt = 0; kt < 2; ++kt) {
+          const int k0 = j0 + 32 * kt;
+          const bool past = k0 + 31 > qw;
+          const bool before = k0 <= qw + 31 - p.window && k0 + 32 > p.sinks;
+          if (!past && !before) continue;
+          const int d0 = qrow - k0 - 4 * hi, d1 = d0 - p.window;
+          if (!before) {
   #pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            const int key = j0 + 32 * kt + 8 * (r / 4) + 4 * hi + (r % 4);
-            if constexpr (WINDOW) {
-              // in the window iff 0 <= qrow - key < window: one unsigned compare
-              bool hidden = (uint32_t)(qrow - key) >= (uint32_t)p.window;
-              if (j0 < p.sinks) hidden &= key >= p.sinks || key > qrow;
-              if (hidden) s[kt][r] = -INFINITY;
+            for (int r = 0; r < 16; ++r)
+              if (8 * (r / 4) + r % 4 > d0) s[kt][r] = -INFINITY;
+          } else {
+            // first keys among these 32, as an offset; and both edges where a window is short
+            const int first = p.sinks - k0 - 4 * hi;
+            if (!past && k0 >= p.sinks) {
+  #pragma unroll
+              for (int r = 0; r < 16; ++r)
+                if (8 * (r / 4) + r % 4 <= d1) s[kt][r] = -INFINITY;
             } else {
+  #pragma unroll
+              for (int r = 0; r < 16; ++r) {
+                const int off = 8 * (r / 4) + r % 4;
+                if (off > d0 || (off <= d1 && off >= first)) s[kt][r] = -INFINITY;
+              }
+            }
+          }
+        }
+      } else {
+        const bool need_mask = (j0 + kBN > N) || (CAUSAL && j0 + kBN - 1 > qw);
+        if (need_mask) {
+  #pragma unroll
+          for (int kt = 0; kt < 2; ++kt) {
+  #pragma unroll
+            for (int r = 0; r < 16; ++r) {
+              const int key = j0 + 32 * kt + 8 * (r / 4) + 4 * hi + (r % 4);
               if (key >= N || (CAUSAL && key > qrow)) s[kt][r] = -INFINITY;
             }
           }
@@ -994,6 +1017,8 @@ __device__ __forceinline__ void attn_fwd_body(const KParams& p) {
       l_run += lsum;
 
       // Straight-line region 2 (not deferred): GEMM-II, O^T += V^T P^T
+      // (WINDOW: not for a block before all of this wave's windows, whose P is 0)
+      if (WINDOW && !DEFER && j0 + kBN <= qw - p.window + 1 && j0 >= p.sinks) return;
       if constexpr (!DEFER) {
   #pragma unroll
         for (int t = 0; t < NV; ++t) {
