@@ -99,6 +99,7 @@
 #include "attn_fwd_launch.h"
 #include "attn_fwd_rules.h"
 #include "tile_order.h"
+#include "window_order.h"
 
 namespace qm {
 namespace {
@@ -426,11 +427,10 @@ enum LayoutSet : int { kBhndOnly = 0, kEitherLayout = 1, kBnhdOnly = 2 };
 // groups' results are merged at the end.
 //
 // WINDOW (with CAUSAL): key j is visible to query i iff j <= i and (j > i - window
-// or j < sinks).  The key loop then walks the blocks that hold first keys and the
-// blocks from the window of the tile's first row on, those between them left out:
-// step j is block j, or j + skip past the first keys' blocks.  A row may see nothing
-// in the first steps; it keeps m = -FLT_MAX and l = O = 0 through them (a masked
-// score's probability is 2^-inf = 0 against any m) until its own window begins.
+// or j < sinks).  The key loop then walks the blocks that some row of the tile sees, in
+// the order of window_order.h.  A row may see nothing in a step; it keeps m, l and O
+// through it (a masked score's probability is 2^-inf = 0 against any m, -FLT_MAX among
+// them).  Against a walk in ascending order: window 512 4-5%, 1024 2%, 4096 -1%.
 template <int DK, int DV, int DT, bool CAUSAL, int WAVES, int G, int LAYOUTS, bool WINDOW = false>
 __device__ __forceinline__ void attn_fwd_body(const KParams& p) {
   using OP = Ops<DT>;
@@ -516,12 +516,15 @@ __device__ __forceinline__ void attn_fwd_body(const KParams& p) {
   i32x4 rk, rv;        // K and V rows of the head
   Frag qf[NKS];        // Q: B operand of GEMM-I, resident for the whole key loop
   int nblk, nkv;       // key blocks of the query block; steps: blocks per group, rounded up
-  int nsink = 0, skip = 0;   // WINDOW: blocks of first keys, and blocks left out after them
+  WindowOrder order;   // WINDOW: the blocks of the steps
   // the key block of this wave's group in step j
   auto key_block = [&](int j) {
     const int i = G > 1 ? j * G + kgrp : j;
-    if constexpr (WINDOW) return i < nsink ? i : i + skip;
-    else return i;
+    if constexpr (WINDOW) {
+      return G > 1 ? order.block_ascending(i) : order.block(i);
+    } else {
+      return i;
+    }
   };
 
   // ---- HBM -> LDS: this wave's load groups of one K or V block ----
@@ -590,10 +593,8 @@ __device__ __forceinline__ void attn_fwd_body(const KParams& p) {
     nblk = (kv_end + kBN - 1) / kBN;
     nkv = (nblk + G - 1) / G;
     if constexpr (WINDOW) {
-      const int first = max(0, qb * BM - p.window + 1) / kBN;   // the block of the first row's window
-      nsink = min(first, (p.sinks + kBN - 1) / kBN);
-      skip = first - nsink;
-      nkv = (nblk - skip + G - 1) / G;
+      order.set(qb * BM, p.window, p.sinks, G > 1);
+      nkv = (order.steps(nblk) + G - 1) / G;
     }
     // lane: query row, k-group (OP::KGB bytes of each k-step)
     const uint32_t q_off = (uint32_t)(qb * BM + wave * 32 + (lane & 31)) * rs_q +
@@ -844,19 +845,19 @@ __device__ __forceinline__ void attn_fwd_body(const KParams& p) {
           if (!before) {
   #pragma unroll
             for (int r = 0; r < 16; ++r)
-              if (8 * (r / 4) + r % 4 > d0) s[kt][r] = -INFINITY;
+              s[kt][r] = 8 * (r / 4) + r % 4 > d0 ? -INFINITY : s[kt][r];
           } else {
             // first keys among these 32, as an offset; and both edges where a window is short
             const int first = p.sinks - k0 - 4 * hi;
             if (!past && k0 >= p.sinks) {
   #pragma unroll
               for (int r = 0; r < 16; ++r)
-                if (8 * (r / 4) + r % 4 <= d1) s[kt][r] = -INFINITY;
+                s[kt][r] = 8 * (r / 4) + r % 4 <= d1 ? -INFINITY : s[kt][r];
             } else {
   #pragma unroll
               for (int r = 0; r < 16; ++r) {
                 const int off = 8 * (r / 4) + r % 4;
-                if (off > d0 || (off <= d1 && off >= first)) s[kt][r] = -INFINITY;
+                s[kt][r] = (off > d0) | ((off <= d1) & (off >= first)) ? -INFINITY : s[kt][r];
               }
             }
           }
@@ -1055,7 +1056,7 @@ __device__ __forceinline__ void attn_fwd_body(const KParams& p) {
     // last row; none for a wave past the sequence end).  It still issues the
     // loads of the blocks after those, and takes every barrier.
     const int b_act =
-        (qw >= N) ? 0 : (CAUSAL ? min(nblk, (qw + 31) / kBN + 1) : nblk) - (WINDOW ? skip : 0);
+        (qw >= N) ? 0 : (CAUSAL ? min(nblk, (qw + 31) / kBN + 1) : nblk) - (order.first - order.nsink);
     const int j_act =
         G > 1 ? __builtin_amdgcn_readfirstlane((unsigned)(b_act - kgrp + G - 1) / G) : b_act;
     // The computed blocks run in one loop and the skipped ones in a second,
