@@ -25,13 +25,14 @@
  *     `dtype` (FP8 calls: one-byte E4M3 codes, bf16 o); otherwise o has the
  *     input type.  lse is a contiguous [B][H][N] float32 array.  Base
  *     pointers must be 16-byte aligned.
- *   - The call validates its arguments on the host, then enqueues one kernel on
+ *   - The call validates its arguments on the host, then enqueues one kernel
+ *     (qm_attn_decode: one or two) on
  *     `stream` (NULL = the null stream) and returns; results are valid once the
  *     caller has synchronised that stream.  On any error nothing is enqueued and
  *     no output is written.
  *   - Calls are thread-safe; calls on different streams may run concurrently,
- *     and calls may be captured into a HIP graph (nothing but the one kernel
- *     launch is enqueued).
+ *     and calls may be captured into a HIP graph (nothing but the kernel
+ *     launches is enqueued).
  *   - Input elements are expected to be finite.  An infinite or NaN element
  *     gives unspecified values in the outputs that read it: its own query row
  *     (an element of q), or every row of the query heads that use its
@@ -92,8 +93,8 @@ enum {
   QM_ERR_TILE = -11,       /* qm_attn_set_tile_rows: rows is not 0, 128 or 256 */
   QM_ERR_WINDOW = -12,     /* window is below 1 (qm_attn_decode: below 0), or sinks below 0 */
   QM_ERR_PAGE = -13,       /* page_size is not a multiple of 16 from 16 to 65536, num_pages,
-                              table_cols or max_length is below 1, or a sequence's table or the
-                              cache is too large to address */
+                              table_cols or max_length is below 1, table_cols * page_size is above
+                              2^29 tokens, or the cache is 2^62 bytes or more */
   QM_ERR_ROTARY = -14,     /* rotary is not a multiple of 16 from 0 to d, its table is missing or
                               (starts NULL) shorter than N, eps is negative, infinite or NaN, or
                               interleaved is neither 0 nor 1 */
@@ -403,7 +404,8 @@ int qm_qk_norm_rope_append(const void* q, const void* k, const void* v, void* q_
  *   q            [in]  device, [B][H][d] of `dtype`.
  *   o            [out] device, [B][H][d] of `dtype`.
  *   lse          [out] device, [B][H] float32, over the visible scaled scores.
- *   lengths      [in]  device, [B] int32: cached tokens of each sequence.  0: o is
+ *   lengths      [in]  device, [B] int32: cached tokens of each sequence, which
+ *                      must not change while the call runs.  0: o is
  *                      0 and lse -infinity.  Below 0, above max_length or beyond the
  *                      page table, or with a page number out of range among the
  *                      visible tokens' pages: that sequence's o and lse are NaN.

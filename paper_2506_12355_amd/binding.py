@@ -273,7 +273,12 @@ def _enqueue(entry, device, stream, before, after) -> None:
     import torch
     index = device.index
     # the current stream's handle alone, without a torch.cuda.Stream object around it
-    raw = torch._C._cuda_getCurrentRawStream(index) if stream is None else stream.cuda_stream
+    if stream is None:
+        raw = torch._C._cuda_getCurrentRawStream(index)
+    elif stream.device.index == index:
+        raw = stream.cuda_stream
+    else:
+        raise ValueError(f"stream must be one of the inputs' device {device}, not of {stream.device}")
     if index == torch.cuda.current_device():
         status = entry(*before, raw, *after)
     else:

@@ -65,6 +65,7 @@ struct Params {
   float* part_o;     // [2 grid][16][d]
   float* part_ml;    // [2 grid][16][2]
   int32_t* desc;     // [rows][2]: first workgroup of a row, and its pieces
+  int grid;          // workgroups of equal shares
   int64_t page_stride;
   uint32_t token_stride, head_stride;
   int num_pages, table_cols;
@@ -451,6 +452,7 @@ __global__ __launch_bounds__(256, 2) void decode_shares_kernel(Params p) {
   while (upto + __builtin_amdgcn_readlane(sum, 63) <= at) {
     upto += __builtin_amdgcn_readlane(sum, 63);
     b += 64;
+    if (b >= p.B) return;   // (only lengths that change under the call get here)
     len = length_of(b + lane);
     sum = running_sum(cost_of(len));
   }
@@ -480,8 +482,8 @@ __global__ __launch_bounds__(256, 2) void decode_shares_kernel(Params p) {
       }
       before = 0;
     }
-    if (left <= 0) return;
-    len = length_of(++b);
+    if (left <= 0 || ++b >= p.B) return;
+    len = length_of(b);
   }
 }
 
@@ -504,7 +506,9 @@ __global__ __launch_bounds__(256) void decode_join_kernel(Params p, int heads) {
   }
   const int hkv = h / p.group, in_group = h - hkv * p.group;
   const int32_t* d = p.desc + 2 * (((size_t)b * p.Hkv + hkv) * p.tiles + in_group / 16);
-  const int first = d[0], pieces = d[1];
+  // (bounded by the partial results there are: lengths that change under the call can
+  // give a row whose numbers were never written)
+  const int first = d[0], pieces = first >= 0 && first < p.grid ? min(d[1], p.grid - first) : 0;
   if (pieces <= 1) return;
   float m = -FLT_MAX, l = 0.f;
   f32x4 o = f32x4{};
@@ -576,6 +580,7 @@ hipError_t launch_width(const DecodeArgs& a, const DecodePlan& plan, hipStream_t
   p.B = a.B, p.H = a.H, p.Hkv = a.Hkv, p.group = a.H / a.Hkv, p.tiles = (p.group + 15) / 16;
   p.limit = a.limit, p.window = a.window, p.sinks = a.sinks;
   p.c = a.c, p.v_scale = a.v_scale;
+  p.grid = plan.grid;
   p.part_o = a.workspace;
   p.part_ml = p.part_o + (size_t)2 * plan.grid * 16 * a.d;
   p.desc = reinterpret_cast<int32_t*>(p.part_ml + (size_t)2 * plan.grid * 16 * 2);

@@ -3,6 +3,7 @@
 
 #include "qm_attn.h"
 
+#include <atomic>
 #include <float.h>
 #include <limits.h>
 #include <math.h>
@@ -34,6 +35,9 @@ bool any_overlap(const Range& out, const Range (&with)[N]) {
 }
 
 constexpr uint64_t kMost = 1ull << 62;   // bytes or elements of a tensor
+// Tokens that a page table can hold for a sequence: 64 sequences' 32-token blocks are
+// counted in 32 bits.
+constexpr int64_t kMostTokens = 1ll << 29;
 
 // a * b, or kMost where that is larger
 uint64_t times(uint64_t a, uint64_t b) {
@@ -45,7 +49,7 @@ int check_cache(qm::PagedCache* c, uint64_t* bytes, int Hkv, int d, int num_page
                 int table_cols, int dtype, int cache_dtype, int cache_layout) {
   if (num_pages < 1 || table_cols < 1 || page_size < 16 || page_size % 16 || page_size > 65536)
     return QM_ERR_PAGE;
-  if ((int64_t)table_cols * page_size > INT_MAX) return QM_ERR_PAGE;
+  if ((int64_t)table_cols * page_size > kMostTokens) return QM_ERR_PAGE;
   if (cache_dtype != dtype && cache_dtype != QM_E4M3) return QM_ERR_DTYPE;
   if (cache_layout != QM_BHND && cache_layout != QM_BNHD) return QM_ERR_LAYOUT;
   const uint64_t es = cache_dtype == QM_E4M3 ? 1 : 2;
@@ -182,6 +186,18 @@ int norm_rope(const void* q, const void* k, const void* v, void* q_out, void* k_
   return qm::launch_norm_rope(a, stream) == hipSuccess ? QM_OK : QM_ERR_LAUNCH;
 }
 
+// CUs of the current device (asked once for each of the first 64), or 0.
+int device_cus() {
+  static std::atomic<int> known[64];
+  int id = 0, cus = 0;
+  if (hipGetDevice(&id) != hipSuccess) return 0;
+  if (id >= 0 && id < 64) cus = known[id].load(std::memory_order_relaxed);
+  if (cus > 0) return cus;
+  if (hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, id) != hipSuccess) return 0;
+  if (id >= 0 && id < 64) known[id].store(cus, std::memory_order_relaxed);
+  return cus;
+}
+
 // Checks of sizes that a decode call and its workspace share, and the call's split.
 int plan(int B, int H, int Hkv, int d, int page_size, int table_cols, int max_length, int window,
          int sinks, qm::DecodePlan* p, int* limit) {
@@ -190,16 +206,14 @@ int plan(int B, int H, int Hkv, int d, int page_size, int table_cols, int max_le
   if (table_cols < 1 || page_size < 16 || page_size % 16 || page_size > 65536 || max_length < 1)
     return QM_ERR_PAGE;
   const int64_t capacity = (int64_t)table_cols * page_size;
-  if (capacity > INT_MAX) return QM_ERR_PAGE;
+  if (capacity > kMostTokens) return QM_ERR_PAGE;
   if (window < 0 || sinks < 0) return QM_ERR_WINDOW;
   *limit = (int)(max_length < capacity ? max_length : capacity);
   const uint64_t tiles = ((uint64_t)(H / Hkv) + 15) / 16;
   const uint64_t rows = times(times((uint64_t)B, (uint64_t)Hkv), tiles);
   if (rows > INT_MAX / 512 || times((uint64_t)B, (uint64_t)H) > INT_MAX / 256) return QM_ERR_SHAPE;
-  int id = 0, cus = 0;
-  if (hipGetDevice(&id) != hipSuccess ||
-      hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, id) != hipSuccess)
-    return QM_ERR_LAUNCH;
+  const int cus = device_cus();
+  if (cus < 1) return QM_ERR_LAUNCH;
   *p = qm::plan_decode((int64_t)rows, qm::decode_blocks(*limit, window, sinks), cus);
   return QM_OK;
 }

@@ -175,3 +175,18 @@ def test_host_tensors_are_refused():
                  lambda: qa.decode(x[:, :, 0], cache, cache, table, table[0]), lambda: qa.fwd_window(x, x, x, 2)):
         with pytest.raises(ValueError, match="ROCm device"):
             call()
+
+
+def test_a_stream_of_another_device_is_refused():
+    torch = pytest.importorskip("torch")
+    from paper_2506_12355_amd import binding
+
+    class Stream:
+        device = torch.device("cuda", 1)
+        cuda_stream = 7
+
+    def entry(*args):
+        raise AssertionError("the library was called")
+
+    with pytest.raises(ValueError, match="stream must be"):
+        binding._enqueue(entry, torch.device("cuda", 0), Stream(), (), ())
