@@ -279,7 +279,7 @@ def _enqueue(entry, device, stream, before, after) -> None:
         raw = stream.cuda_stream
     else:
         raise ValueError(f"stream must be one of the inputs' device {device}, not of {stream.device}")
-    if index == torch.cuda.current_device():
+    if index == torch._C._cuda_getDevice():   # (torch.cuda.current_device, without its checks)
         status = entry(*before, raw, *after)
     else:
         with torch.cuda.device(index):

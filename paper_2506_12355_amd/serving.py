@@ -25,8 +25,8 @@ _MOST = 2 ** 31 - 1   # no bound on lengths but the page table's
 
 
 # The checks below read each property of a tensor once and put off what a message needs
-# until there is one: a call of one token takes the GPU a few microseconds, and its
-# arguments took the host 11 (now 6; allocating the outputs and the launch come on top).
+# until there is one: a call of one token takes the GPU a few microseconds, less than its
+# arguments take the host.
 
 def _layout_code(layout, name="layout"):
     code = _LAYOUTS.get(layout)
@@ -70,25 +70,38 @@ def _rows(name, t, dtype, index, layout):
     return size, _Strides(s[0], s[1], s[2]) if layout else _Strides(s[0], s[2], s[1])
 
 
-def _vector(name, t, size, index, dtype):
-    """The address of a contiguous tensor of `size`, or None for None."""
-    if t is None:
-        return None
-    if t.shape != size or t.dtype is not dtype or not t.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous {list(size)} tensor of {dtype}")
+def _misfit(name, t, size, index, dtype):
     if t.get_device() != index:
-        raise _elsewhere(name, t, index)
+        return _elsewhere(name, t, index)
+    return ValueError(f"{name} must be a contiguous {list(size)} tensor of {dtype}")
+
+
+def _vectors(names, a, b, size, index, dtype):
+    """The addresses of two contiguous tensors of `size`, None for None."""
+    if a is not None:
+        if a.shape != size or a.dtype is not dtype or a.get_device() != index or not a.is_contiguous():
+            raise _misfit(names[0], a, size, index, dtype)
+        a = a.data_ptr()
+    if b is not None:
+        if b.shape != size or b.dtype is not dtype or b.get_device() != index or not b.is_contiguous():
+            raise _misfit(names[1], b, size, index, dtype)
+        b = b.data_ptr()
+    return a, b
+
+
+def _vector(name, t, size, index, dtype):
+    """The address of a contiguous tensor of `size`."""
+    if t.shape != size or t.dtype is not dtype or t.get_device() != index or not t.is_contiguous():
+        raise _misfit(name, t, size, index, dtype)
     return t.data_ptr()
 
 
-def _output(name, out, like, index):
-    """The caller's output, checked, or a new contiguous tensor shaped like `like`."""
-    if out is None:
-        if type(like) is _torch().Tensor and like.is_contiguous():
-            return _torch().empty_like(like)
-        return _torch().empty(like.shape, dtype=like.dtype, device=like.device)
-    _vector(name, out, like.shape, index, like.dtype)
-    return out
+def _new(torch, like):
+    """A new contiguous tensor shaped like `like` (empty_like is the shorter call, but
+    keeps a subclass and strides)."""
+    if type(like) is torch.Tensor and like.is_contiguous():
+        return torch.empty_like(like)
+    return torch.empty(like.shape, dtype=like.dtype, device=like.device)
 
 
 def _angles(cos, sin, index):
@@ -100,9 +113,7 @@ def _angles(cos, sin, index):
     size = cos.shape
     if len(size) != 2 or sin.shape != size:
         raise ValueError("cos and sin must have shape [positions, rotary / 2]")
-    f32 = _torch().float32
-    return (_vector("cos", cos, size, index, f32), _vector("sin", sin, size, index, f32),
-            2 * size[1], size[0])
+    return (*_vectors(("cos", "sin"), cos, sin, size, index, _torch().float32), 2 * size[1], size[0])
 
 
 @functools.lru_cache(maxsize=1)
@@ -117,7 +128,8 @@ def _device(index):
 
 
 def _cache(k_cache, v_cache, page_table, B, d, dtype, code, index, cache_layout):
-    """Cache arguments, checked: (num_pages, page_size, heads, columns, cache type, layout)."""
+    """Cache arguments, checked: (num_pages, page_size, heads, columns, the page table's
+    address, cache type, layout)."""
     layout = _layout_code(cache_layout, "cache_layout")
     size, kind = k_cache.shape, k_cache.dtype
     if len(size) != 4 or v_cache.shape != size:
@@ -138,11 +150,11 @@ def _cache(k_cache, v_cache, page_table, B, d, dtype, code, index, cache_layout)
         heads, page_size = page_size, heads
     if width != d:
         raise ValueError("the cache must have the queries' width")
-    table = page_table.shape
-    if len(table) != 2 or table[0] != B:
+    columns = page_table.shape
+    if len(columns) != 2 or columns[0] != B:
         raise ValueError("page_table must have shape [B, columns]")
-    _vector("page_table", page_table, table, index, _torch().int32)
-    return pages, page_size, heads, table[1], code, layout
+    table = _vector("page_table", page_table, columns, index, _torch().int32)
+    return pages, page_size, heads, columns[1], table, code, layout
 
 
 def qk_norm_rope(q, k, cos=None, sin=None, q_weight=None, k_weight=None, eps: float = 1e-6,
@@ -171,16 +183,21 @@ def qk_norm_rope(q, k, cos=None, sin=None, q_weight=None, k_weight=None, eps: fl
     if Bk != B or Nk != N or dk != d:
         raise ValueError("k must match q in B, N and d")
     c, s, rotary, table_rows = _angles(cos, sin, index)
-    i32, sequences, columns = _torch().int32, (B,), (d,)
-    args = (_vector("q_weight", q_weight, columns, index, dtype),
-            _vector("k_weight", k_weight, columns, index, dtype), c, s,
-            _vector("starts", starts, sequences, index, i32),
-            _vector("counts", counts, sequences, index, i32),
-            B, H, Hkv, N, d, rotary, table_rows, float(eps), 1 if interleaved else 0, qs, ks)
-    q_out = _output("q_out", q_out, q, index)
-    k_out = _output("k_out", k_out, k, index)
+    torch = _torch()
+    qw, kw = _vectors(("q_weight", "k_weight"), q_weight, k_weight, (d,), index, dtype)
+    first, held = _vectors(("starts", "counts"), starts, counts, (B,), index, torch.int32)
+    if q_out is None:
+        q_out = _new(torch, q)
+    else:
+        _vector("q_out", q_out, q.shape, index, dtype)
+    if k_out is None:
+        k_out = _new(torch, k)
+    else:
+        _vector("k_out", k_out, k.shape, index, dtype)
     _enqueue(load_library().qm_qk_norm_rope, _device(index), stream,
-             (q.data_ptr(), k.data_ptr(), q_out.data_ptr(), k_out.data_ptr()) + args, (code, lay))
+             (q.data_ptr(), k.data_ptr(), q_out.data_ptr(), k_out.data_ptr(), qw, kw, c, s, first,
+              held, B, H, Hkv, N, d, rotary, table_rows, float(eps), 1 if interleaved else 0, qs, ks),
+             (code, lay))
     return q_out, k_out
 
 
@@ -207,23 +224,24 @@ def qk_norm_rope_append(q, k, v, k_cache, v_cache, page_table, starts=None, cos=
     if Bk != B or Nk != N or dk != d or size_v != (B, N, Hkv, d):
         raise ValueError("k and v must have one shape and match q in B, N and d")
     c, s, rotary, table_rows = _angles(cos, sin, index)
-    pages, page_size, heads, table_columns, kind, cache_lay = _cache(
+    pages, page_size, heads, table_columns, table, kind, cache_lay = _cache(
         k_cache, v_cache, page_table, B, d, dtype, code, index, cache_layout)
     if heads != Hkv:
         raise ValueError("the cache must have the keys' heads")
-    i32, sequences, columns = _torch().int32, (B,), (d,)
-    args = (k_cache.data_ptr(), v_cache.data_ptr(), page_table.data_ptr(),
-            _vector("q_weight", q_weight, columns, index, dtype),
-            _vector("k_weight", k_weight, columns, index, dtype), c, s,
-            _vector("starts", starts, sequences, index, i32),
-            _vector("counts", counts, sequences, index, i32),
-            B, H, Hkv, N, d, rotary, table_rows, float(eps), 1 if interleaved else 0,
-            pages, page_size, table_columns, float(k_scale), float(v_scale), qs, ks, vs)
-    q_out = _output("q_out", q_out, q, index)
+    torch = _torch()
+    qw, kw = _vectors(("q_weight", "k_weight"), q_weight, k_weight, (d,), index, dtype)
+    first, held = _vectors(("starts", "counts"), starts, counts, (B,), index, torch.int32)
+    if q_out is None:
+        q_out = _new(torch, q)
+    else:
+        _vector("q_out", q_out, q.shape, index, dtype)
     if k_out is not None:
-        k_out = _output("k_out", k_out, k, index).data_ptr()
+        k_out = _vector("k_out", k_out, k.shape, index, dtype)
     _enqueue(load_library().qm_qk_norm_rope_append, _device(index), stream,
-             (q.data_ptr(), k.data_ptr(), v.data_ptr(), q_out.data_ptr(), k_out) + args,
+             (q.data_ptr(), k.data_ptr(), v.data_ptr(), q_out.data_ptr(), k_out, k_cache.data_ptr(),
+              v_cache.data_ptr(), table, qw, kw, c, s, first, held, B, H, Hkv, N, d, rotary,
+              table_rows, float(eps), 1 if interleaved else 0, pages, page_size, table_columns,
+              float(k_scale), float(v_scale), qs, ks, vs),
              (code, lay, kind, cache_lay))
     return q_out
 
@@ -247,7 +265,7 @@ def decode_workspace(q, k_cache, page_table, max_length: int | None = None,
     if q.dim() != 3:
         raise ValueError("q must have shape [B, H, d]")
     B, H, d = q.shape
-    _, page_size, heads, columns, _, _ = _cache(k_cache, k_cache, page_table, B, d, dtype, code,
+    _, page_size, heads, columns, _, _, _ = _cache(k_cache, k_cache, page_table, B, d, dtype, code,
                                                 index, cache_layout)
     return _workspace_bytes(index, B, H, heads, d, page_size, columns,
                             _MOST if max_length is None else _int32(max_length, "max_length"),
@@ -284,7 +302,7 @@ def decode(q, k_cache, v_cache, page_table, lengths, scale: float | None = None,
     if q.dim() != 3 or not q.is_contiguous():
         raise ValueError("q must be a contiguous [B, H, d] tensor")
     B, H, d = q.shape
-    pages, page_size, Hkv, columns, kind, cache_lay = _cache(
+    pages, page_size, Hkv, columns, table, kind, cache_lay = _cache(
         k_cache, v_cache, page_table, B, d, dtype, code, index, cache_layout)
     torch = _torch()
     if lengths is None:
@@ -294,7 +312,10 @@ def decode(q, k_cache, v_cache, page_table, lengths, scale: float | None = None,
     window = 0 if window is None else _window(window)
     sinks = _int32(sinks, "sinks")
     most = _MOST if max_length is None else _int32(max_length, "max_length")
-    out = _output("out", out, q, index)
+    if out is None:
+        out = _new(torch, q)
+    else:
+        _vector("out", out, q.shape, index, dtype)
     if lse is None:
         lse = torch.empty(B, H, dtype=torch.float32, device=_device(index))
     else:
@@ -319,7 +340,7 @@ def decode(q, k_cache, v_cache, page_table, lengths, scale: float | None = None,
         ws, given = None, 0
     _enqueue(load_library().qm_attn_decode, _device(index), stream,
              (q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), out.data_ptr(), lse.data_ptr(),
-              page_table.data_ptr(), lens, B, H, Hkv, d, pages, page_size, columns, most, scale,
+              table, lens, B, H, Hkv, d, pages, page_size, columns, most, scale,
               float(k_scale), float(v_scale), window, sinks, ws, given),
              (code, kind, cache_lay))
     return out, lse
