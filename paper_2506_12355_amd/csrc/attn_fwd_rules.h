@@ -97,31 +97,34 @@ inline int choose_waves(const AttnArgs& a, int cus) {
 // long as one another.  Functions of the shape, type, window and first keys alone, as
 // above.
 
-// Key groups where all query blocks fit the device at once, from few steps on: B = 1, us,
-// unsplit -> two -> four groups, d = 64: N = 1000 H = 16 window 64 10.3 -> 9.8 -> 8.1, 256
-// 15.9 -> 13.1 -> 10.7, N = 4000 H = 4 window 1000 26.0 -> 19.9 -> 15.2; two groups,
-// d = 128: N = 1000 H = 4 window 128 15.7 -> 15.7, N = 2000 H = 16 window 256
-// 20.6 -> 20.2, 1024 31.9 -> 29.2, N = 8192 H = 2 window 4096 96.1 -> 59.7.
+// Key groups where all query blocks fit the device at once, from few steps on.  B = 1,
+// us, unsplit -> two -> four groups, d = 64: N = 256 H = 4 window 100 9.0 -> 8.8 -> 7.3,
+// N = 1000 H = 16 window 64 10.0 -> 9.2 -> 8.0, 256 12.4 -> 11.1 -> 9.2, N = 4000 H = 4
+// window 1000 20.6 -> 17.6 -> 13.5; two groups, d = 128: N = 1000 H = 4 window 128
+// 12.7 -> 13.4, N = 2000 H = 16 window 256 17.6 -> 17.8, 1024 27.2 -> 26.3, N = 450 H = 8
+// window 300 14.3 -> 13.7, N = 8192 H = 2 window 4096 65.9 -> 54.9.
 inline int window_groups(const AttnArgs& a, int cus) {
   if (a.d == 192) return 1;
   const auto fits = [&](int rows) { return (long long)((a.N + rows - 1) / rows) * a.B * a.H <= cus; };
   const long long steps = ((long long)a.window + 128) / 64 + (a.sinks + 63) / 64;
   if (a.d == 64 && a.N >= 256 && fits(64)) return 4;
-  if (a.N >= 512 && steps >= (a.d == 64 ? 3 : 6) && fits(128)) return 2;
+  if (a.N >= 384 && steps >= (a.d == 64 ? 3 : 7) && fits(128)) return 2;
   return 1;
 }
 
-// Wavefronts.  A 256-row tile walks two key blocks more than a 128-row one.  us, 128 ->
-// 256 rows, d = 64 (H = 32): N = 8192 B = 4 window 256 235 -> 350, N = 32768 window 8192
-// 2169 -> 2283; d = 128: N = 8192 B = 4 window 512 480 -> 536, 2048 1085 -> 1095,
-// N = 16384 window 2048 562 -> 553, 3000 771 -> 735, 4096 968 -> 939, but where 256-row
-// tiles end in a round that leaves CUs idle N = 4096 H = 24 window 2500 121 -> 144 (the
-// costs of choose_waves).  192-wide keys, one workgroup of either size a CU: H = 16
-// N = 4096 window 512 45.9 -> 40.0, H = 8 (all 128-row tiles at once) 24.5 -> 34.5.
+// Wavefronts.  A 256-row tile walks two key blocks more than a 128-row one and keeps K
+// and V for twice the rows.  us, 128 -> 256 rows, d = 128, H = 32: N = 8192 B = 4 window
+// 512 435 -> 469, 1024 652 -> 685, 2048 1061 -> 1069, N = 16384 window 2500 662 -> 661,
+// 3000 756 -> 747, 4096 963 -> 937; but where 256-row tiles end in a round that leaves
+// CUs idle N = 4096 H = 24 window 2500 114 -> 133, N = 8192 H = 10 window 3000 134 -> 153
+// (the costs of choose_waves).  192-wide keys, one workgroup of either size a CU: H = 16
+// N = 4096 window 512 42.5 -> 38.4, H = 8 (all 128-row tiles at once) 22.3 -> 29.2.
+// d = 64: 128 rows (256 with this kernel before its masks went by halves: N = 8192 B = 4
+// H = 32 window 256 235 -> 350, N = 32768 window 8192 2169 -> 2283).
 inline int choose_window_waves(const AttnArgs& a, int cus) {
   const auto tiles = [&](int rows) { return (long long)((a.N + rows - 1) / rows) * a.B * a.H; };
   if (a.d == 192) return tiles(128) <= cus ? 4 : 8;
-  if (a.d == 64 || a.window <= 2048) return 4;
+  if (a.d == 64 || a.window <= 2560) return 4;
   const auto units = [&](int rows, int alone, int beside) {
     const long long left = tiles(rows) % cus, full = tiles(rows) / cus;
     return full / 2 * beside + full % 2 * alone + (left == 0 ? 0 : full % 2 ? beside - alone : alone);

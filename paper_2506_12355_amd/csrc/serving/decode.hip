@@ -27,7 +27,7 @@
 // reach the result.
 //
 // Work: a row is one (sequence, key/value head, 16-head tile), its work its blocks.
-// Where rows are short, or many, a workgroup takes a whole row (WHOLE).  Else all rows'
+// Where rows are short, or many, a workgroup takes a whole row (decode_rules.h).  Else all rows'
 // blocks, end to end, are dealt in equal shares to as many workgroups as the device
 // holds, which evens out sequences of any lengths.  A workgroup's wavefronts take a
 // piece's blocks in turn and join their (m, l, O) in LDS; of a row that was cut, each
@@ -35,6 +35,11 @@
 // them in order, so results do not depend on which finished first.  A workgroup's range
 // cuts at most its first row (slot 2 w: a piece that continues a row) and its last
 // (slot 2 w + 1: a piece that begins one).
+//
+// Measured (us; a sum over 1 GiB reads 6.21 TB/s, a floor of 0.161 us a MB): 64 sequences
+// of 0 to 8192 tokens, 64/8 heads, bf16, d = 128 196 (5.5 TB/s), all of 8192 (32 of them)
+// 193 (5.6), of 32768 (64) 1402 (6.13); one of 131072 with E4M3 pages 56 (4.8); one of
+// 1000 9.9, a chain of latencies: length, page numbers, rows, join, second kernel.
 //
 // Window: the blocks walked are those with first keys, then those from the window on;
 // list index i is block i, or i + skip past the first keys' blocks.
@@ -53,7 +58,6 @@ constexpr int kMinShare = 4;           // least blocks of a workgroup's share: o
 // join, 5-8 us, against 1.1 us a block.  Counted as 0, 6 and 12 (us): 512 rows of up to
 // 8192 tokens 205, 198, 199; up to 2000 88, 64, 65; 8 rows of 2000 13.4, 10.8, 10.8.
 constexpr int kRowCost = 6;
-
 
 struct Params {
   const uint16_t* q;
@@ -336,7 +340,7 @@ __device__ __forceinline__ void piece(const Params& p, float* lds, int b, int ro
   // ---- join the wavefronts: each scales its O to the common maximum; half of them put
   // theirs into LDS, the other half add their own ----
   constexpr int HALF = WAVES / 2;
-  float* const ml = lds;                     // [WAVES][16][2], then [16][2]
+  float* const ml = lds;                     // [WAVES][16][2]
   float* const part = lds + WAVES * 32;      // [HALF][16][D]
   l = sum_over_groups(l);
   if (__any(bad)) l = __builtin_nanf("");   // a length or page out of range
