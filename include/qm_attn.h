@@ -352,7 +352,7 @@ int qm_attn_set_tile_rows(int rows);
  *                      zeros, whatever their input holds.
  *   d            64 or 128.       rotary   0, or a multiple of 16 up to d.
  *   A token whose position is outside the table gets NaN rows.
- *   Hkv need not divide H.
+ *   Hkv need not divide H.  B * N * (H + 2 Hkv) is below 2^27 (QM_ERR_SHAPE).
  *   stream, errors, capture: as for the calls above (one kernel, nothing else).
  */
 int qm_qk_norm_rope(const void* q, const void* k, void* q_out, void* k_out,
@@ -409,7 +409,7 @@ int qm_qk_norm_rope_append(const void* q, const void* k, const void* v, void* q_
  *                      0 and lse -infinity.  Below 0, above max_length or beyond the
  *                      page table, or with a page number out of range among the
  *                      visible tokens' pages: that sequence's o and lse are NaN.
- *   d            64 or 128.  H % Hkv == 0.
+ *   d            64 or 128.  H % Hkv == 0.  B * H is below 2^22 (QM_ERR_SHAPE).
  *   max_length   a bound on lengths that the host knows; the call's split of the
  *                cache is chosen for it (and for the number of sequences), so a close
  *                one is faster.
