@@ -6,6 +6,7 @@ There is no fallback: if ``libqm_attn.so`` is missing, loading fails loudly.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import operator
 import os
@@ -222,11 +223,12 @@ def fwd_fp8(q, k, v, scales, causal: bool = False, scale: float | None = None, o
     if v.shape != k.shape or Bk != B or Nk != N or dk != d:
         raise ValueError("k and v must hold Hkv heads matching q in B, N and d")
     scale = 1.0 / d ** 0.5 if scale is None else float(scale)   # rounded to float32 by the call
-    if out is None:
-        out = torch.empty(q.shape, dtype=torch.bfloat16, device=device)
-    elif out.shape != q.shape or out.dtype != torch.bfloat16 or not out.is_contiguous():
-        raise ValueError("out must be a contiguous bfloat16 tensor shaped like q")
-    lse = _lse(q, lse, B, H, N)
+    with _pool_of(stream, out is None or lse is None):
+        if out is None:
+            out = torch.empty(q.shape, dtype=torch.bfloat16, device=device)
+        elif out.shape != q.shape or out.dtype != torch.bfloat16 or not out.is_contiguous():
+            raise ValueError("out must be a contiguous bfloat16 tensor shaped like q")
+        lse = _lse(q, lse, B, H, N)
     _check_outputs_on(device, out, lse)
     qs, ks, vs = (float(t) for t in scales)
     args = (q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), lse.data_ptr(), B, H)
@@ -255,6 +257,18 @@ def _check_outputs_on(device, out, lse) -> None:
     for name, t in (("out", out), ("lse", lse)):
         if not t.is_cuda or t.device != device:
             raise ValueError(f"{name} must be on the inputs' device {device}, not {t.device}")
+
+
+_CURRENT = contextlib.nullcontext()
+
+
+def _pool_of(stream, new):
+    """A context that takes new tensors, where there are any, from the pool of the stream
+    that the call runs on.  From the current stream's pool, beside a `stream` of the
+    caller's, their memory could still be in use by that stream's earlier work, and be given
+    out to its later work while the kernel writes it: nothing orders the two."""
+    import torch
+    return torch.cuda.stream(stream) if new and stream is not None else _CURRENT
 
 
 def _lse(q, lse, B, H, N):
@@ -297,7 +311,7 @@ def _dtype_code(t) -> int:
     raise TypeError(f"q, k, v must be float16 or bfloat16, not {t.dtype}")
 
 
-def _checked(q, k, v, scale, out, lse, layout):
+def _checked(q, k, v, scale, out, lse, stream, layout):
     """The checks that the 16-bit calls share.  Returns (the C arguments up to the
     query heads, Hkv, N, d, dv, scale, dtype code, o, lse)."""
     import torch
@@ -328,17 +342,18 @@ def _checked(q, k, v, scale, out, lse, layout):
     code = _dtype_code(q)
     # the C float argument rounds the scale to float32
     scale = 1.0 / d ** 0.5 if scale is None else float(scale)
-    if out is None:
-        # (empty_like is a microsecond shorter, but would keep a subclass)
-        if dv == d and type(q) is torch.Tensor:
-            out = torch.empty_like(q)
+    with _pool_of(stream, out is None or lse is None):
+        if out is None:
+            # (empty_like is a microsecond shorter, but would keep a subclass)
+            if dv == d and type(q) is torch.Tensor:
+                out = torch.empty_like(q)
+            else:
+                out = torch.empty((*qs[:3], dv), dtype=q.dtype, device=q.device)
         else:
-            out = torch.empty((*qs[:3], dv), dtype=q.dtype, device=q.device)
-    else:
-        oshape = (*qs[:3], dv)
-        if tuple(out.shape) != oshape or out.dtype != q.dtype or not out.is_contiguous():
-            raise ValueError(f"out must be a contiguous {list(oshape)} tensor of q's dtype")
-    lse = _lse(q, lse, B, H, N)
+            oshape = (*qs[:3], dv)
+            if tuple(out.shape) != oshape or out.dtype != q.dtype or not out.is_contiguous():
+                raise ValueError(f"out must be a contiguous {list(oshape)} tensor of q's dtype")
+        lse = _lse(q, lse, B, H, N)
     _check_outputs_on(q.device, out, lse)
     args = (q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), lse.data_ptr(), B, H)
     return args, Hkv, N, d, dv, scale, code, out, lse
@@ -356,9 +371,12 @@ def fwd(q, k, v, causal: bool = False, scale: float | None = None, out=None, lse
     [B, N, H, d], k [B, N, Hkv, d], v [B, N, Hkv, dv], o [B, N, H, dv];
     ``qm_attn_fwd_layout``).  Returns (o, lse): o of q's dtype, lse float32
     [B, H, N] in either layout.  ``scale`` defaults to 1/sqrt(d) rounded to
-    float32.  ``stream`` defaults to the current stream of q's device.
+    float32.  ``stream`` defaults to the current stream of q's device.  Outputs that
+    the call makes are tensors of the stream it runs on: work of another stream waits
+    for it before it reads them, and, as for any tensor of another stream, the inputs and
+    outputs live until the streams that use them are done (``Tensor.record_stream``).
     """
-    args, Hkv, N, d, dv, scale, code, out, lse = _checked(q, k, v, scale, out, lse, layout)
+    args, Hkv, N, d, dv, scale, code, out, lse = _checked(q, k, v, scale, out, lse, stream, layout)
     lib, device = load_library(), q.device
     causal = 1 if causal else 0
     if layout == "bnhd":
@@ -383,7 +401,7 @@ def fwd_window(q, k, v, window: int, sinks: int = 0, scale: float | None = None,
     1); a window that reaches every key gives exactly ``fwd(causal=True)``.
     Tensors, types, the other arguments and the results are those of :func:`fwd`
     (``qm_attn_fwd_window``; key blocks that no query sees cost nothing)."""
-    args, Hkv, N, d, dv, scale, code, out, lse = _checked(q, k, v, scale, out, lse, layout)
+    args, Hkv, N, d, dv, scale, code, out, lse = _checked(q, k, v, scale, out, lse, stream, layout)
     _enqueue(load_library().qm_attn_fwd_window, q.device, stream,
              args + (Hkv, N, d, dv, scale, _int32(window, "window"), _int32(sinks, "sinks")),
              (code, QM_BNHD if layout == "bnhd" else QM_BHND))

@@ -2,7 +2,8 @@
 position rotation, a paged cache of keys and values, and attention of new tokens over it.
 
 As in ``binding``: argument marshalling only, on torch's memory and streams; every step
-runs in the gfx950 kernels of the library (``include/qm_attn.h``).
+runs in the gfx950 kernels of the library (``include/qm_attn.h``).  Outputs and workspaces
+that a call makes are tensors of the stream it runs on (see :func:`binding.fwd`).
 
 The cache is two tensors of pages, [num_pages, Hkv, page_size, d] (``cache_layout``
 "bhnd") or [num_pages, page_size, Hkv, d] ("bnhd"), of the model's 16-bit type or
@@ -15,7 +16,7 @@ import ctypes
 import functools
 
 from .binding import (QM_BHND, QM_BNHD, QM_OK, QmAttnError, _dtype_code, _enqueue, _int32,
-                      load_library, strerror)
+                      _pool_of, load_library, strerror)
 
 QM_E4M3 = 2   # qm_dtype_t: cached keys and values
 
@@ -186,14 +187,15 @@ def qk_norm_rope(q, k, cos=None, sin=None, q_weight=None, k_weight=None, eps: fl
     torch = _torch()
     qw, kw = _vectors(("q_weight", "k_weight"), q_weight, k_weight, (d,), index, dtype)
     first, held = _vectors(("starts", "counts"), starts, counts, (B,), index, torch.int32)
-    if q_out is None:
-        q_out = _new(torch, q)
-    else:
-        _vector("q_out", q_out, q.shape, index, dtype)
-    if k_out is None:
-        k_out = _new(torch, k)
-    else:
-        _vector("k_out", k_out, k.shape, index, dtype)
+    with _pool_of(stream, q_out is None or k_out is None):
+        if q_out is None:
+            q_out = _new(torch, q)
+        else:
+            _vector("q_out", q_out, q.shape, index, dtype)
+        if k_out is None:
+            k_out = _new(torch, k)
+        else:
+            _vector("k_out", k_out, k.shape, index, dtype)
     _enqueue(load_library().qm_qk_norm_rope, _device(index), stream,
              (q.data_ptr(), k.data_ptr(), q_out.data_ptr(), k_out.data_ptr(), qw, kw, c, s, first,
               held, B, H, Hkv, N, d, rotary, table_rows, float(eps), 1 if interleaved else 0, qs, ks),
@@ -232,7 +234,8 @@ def qk_norm_rope_append(q, k, v, k_cache, v_cache, page_table, starts=None, cos=
     qw, kw = _vectors(("q_weight", "k_weight"), q_weight, k_weight, (d,), index, dtype)
     first, held = _vectors(("starts", "counts"), starts, counts, (B,), index, torch.int32)
     if q_out is None:
-        q_out = _new(torch, q)
+        with _pool_of(stream, True):
+            q_out = _new(torch, q)
     else:
         _vector("q_out", q_out, q.shape, index, dtype)
     if k_out is not None:
@@ -312,32 +315,27 @@ def decode(q, k_cache, v_cache, page_table, lengths, scale: float | None = None,
     window = 0 if window is None else _window(window)
     sinks = _int32(sinks, "sinks")
     most = _MOST if max_length is None else _int32(max_length, "max_length")
-    if out is None:
-        out = _new(torch, q)
-    else:
-        _vector("out", out, q.shape, index, dtype)
-    if lse is None:
-        lse = torch.empty(B, H, dtype=torch.float32, device=_device(index))
-    else:
-        _vector("lse", lse, (B, H), index, torch.float32)
-    need = _workspace_bytes(index, B, H, Hkv, d, page_size, columns, most, window, sinks)
-    if workspace is not None:
-        if workspace.dtype is not torch.uint8 or workspace.dim() != 1 or not workspace.is_contiguous():
-            raise ValueError("workspace must be a contiguous 1-D uint8 tensor")
-        if workspace.get_device() != index:
-            raise _elsewhere("workspace", workspace, index)
-        ws, given = workspace.data_ptr(), workspace.numel()
-    elif need:
-        # from the pool of the stream that will use it: freed on return, its memory is
-        # given out again in that stream's order only
-        if stream is None:
-            workspace = torch.empty(need, dtype=torch.uint8, device=_device(index))
+    with _pool_of(stream, out is None or lse is None or workspace is None):
+        if out is None:
+            out = _new(torch, q)
         else:
-            with torch.cuda.stream(stream):
-                workspace = torch.empty(need, dtype=torch.uint8, device=_device(index))
-        ws, given = workspace.data_ptr(), need
-    else:
-        ws, given = None, 0
+            _vector("out", out, q.shape, index, dtype)
+        if lse is None:
+            lse = torch.empty(B, H, dtype=torch.float32, device=_device(index))
+        else:
+            _vector("lse", lse, (B, H), index, torch.float32)
+        need = _workspace_bytes(index, B, H, Hkv, d, page_size, columns, most, window, sinks)
+        if workspace is not None:
+            if workspace.dtype is not torch.uint8 or workspace.dim() != 1 or not workspace.is_contiguous():
+                raise ValueError("workspace must be a contiguous 1-D uint8 tensor")
+            if workspace.get_device() != index:
+                raise _elsewhere("workspace", workspace, index)
+            ws, given = workspace.data_ptr(), workspace.numel()
+        elif need:
+            workspace = torch.empty(need, dtype=torch.uint8, device=_device(index))
+            ws, given = workspace.data_ptr(), need
+        else:
+            ws, given = None, 0
     _enqueue(load_library().qm_attn_decode, _device(index), stream,
              (q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), out.data_ptr(), lse.data_ptr(),
               table, lens, B, H, Hkv, d, pages, page_size, columns, most, scale,
