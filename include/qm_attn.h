@@ -420,12 +420,12 @@ int qm_qk_norm_rope_append(const void* q, const void* k, const void* v, void* q_
  *                before the call does not matter, and after it is unspecified; calls
  *                that may run at once must not share one.
  *
- * Arithmetic as in qm_attn_fwd (E4M3 codes are widened exactly; the probabilities
- * are rounded to `dtype` before the second product).  What the cache holds in
- * places that are not visible does not matter, NaN included.  Results are
- * deterministic; a sequence's bytes may depend on B, the other sequences' lengths,
- * max_length and the device's CU count, within the rounding of fp32 sums (where its
- * cache is cut between workgroups).  One kernel is enqueued, or two.
+ * Arithmetic in fp32 (E4M3 codes are widened exactly; the probabilities enter the
+ * second product as two values of `dtype`, which lose 2^-16 (bf16) or 2^-22 (fp16) of
+ * them).  What the cache holds in places that are not visible does not matter, NaN
+ * included.  Results are deterministic; a sequence's bytes may depend on B, the other
+ * sequences' lengths, max_length and the device's CU count, within the rounding of fp32
+ * sums (where its cache is cut between workgroups).  One kernel is enqueued, or two.
  */
 int qm_attn_decode(const void* q, const void* k_cache, const void* v_cache, void* o, float* lse,
                    const int* page_table, const int* lengths, int B, int H, int Hkv, int d,

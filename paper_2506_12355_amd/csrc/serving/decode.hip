@@ -18,9 +18,15 @@
 //
 // The order of the contraction and of the M tiles is free, so neither K, V nor P moves
 // between lanes.  E4M3 codes are widened to the query's type on the way (exact) and
-// take the same path.  Scores, maxima and sums are in fp32, base 2 (c = scale log2 e);
-// P is rounded to the query's 16-bit type for the second product, as the package's
-// other attention kernels round it: the row sum keeps the unrounded values.
+// take the same path.  Scores, maxima and sums are in fp32, base 2 (c = scale log2 e).
+// P enters the second product as two values of the query's 16-bit type, P rounded and
+// what that left, one MFMA each: 2^-16 (bf16) or 2^-22 (f16) of a weight is lost, where
+// one value loses 2^-8 or 2^-11, as much as the rounding of O.  The wavefronts wait for
+// memory, so that the second MFMA costs little (us, one value -> two: 64 sequences of 0 to
+// 8192 tokens 196.6 -> 197.2, one of 131072 in E4M3 58.4 -> 58.6, one of 1000 10.1 -> 10.3).
+// f16's smallest step is 2^-24: there the operands are 2^15 times the weights (kWeight),
+// the largest of which is 1, so that of those far below it 2^-40 each is lost.  Row sums
+// take the weights in fp32.
 //
 // Keys that are hidden (past the length, or before the window and past the first keys)
 // get the score -inf and a zero V row: what their memory holds, NaN included, does not
@@ -54,6 +60,9 @@ namespace {
 
 constexpr int kBlock = kDecodeBlock;   // tokens of a wavefront's step
 constexpr int kMinShare = 4;           // least blocks of a workgroup's share: one a wavefront
+// The second product's factor (see above); O is divided by it at the end.
+template <int DT>
+constexpr float kWeight = DT == 0 ? 32768.f : 1.f;
 // What a row costs a workgroup beside its blocks, in blocks: its first loads and its
 // join, 5-8 us, against 1.1 us a block.  Counted as 0, 6 and 12 (us): 512 rows of up to
 // 8192 tokens 205, 198, 199; up to 2000 88, 64, 65; 8 rows of 2000 13.4, 10.8, 10.8.
@@ -142,11 +151,11 @@ struct Raw<8> { using T = u32x2; };
 template <>
 struct Raw<4> { using T = uint32_t; };
 
-// Four columns of a finished row: O = sum / l, and lse.  No visible token (l = 0) gives
+// Four columns of a finished row: O = sum / (kWeight l), and lse.  No visible token (l = 0) gives
 // O = 0 and lse = -inf.
 template <int DT>
 __device__ __forceinline__ void finish(const Params& p, size_t row, int d, int col, f32x4 sum, float m, float l) {
-  sum *= l == 0.f ? 0.f : p.v_scale / l;
+  sum *= l == 0.f ? 0.f : p.v_scale * (1.f / kWeight<DT>) / l;
   *reinterpret_cast<u32x2*>(p.o + row * d + col) =
       u32x2{Type16<DT>::pack(sum[0], sum[1]), Type16<DT>::pack(sum[2], sum[3])};
   if (col == 0) p.lse[row] = (m + log2f(l)) * 0.69314718055994531f;
@@ -300,9 +309,14 @@ __device__ __forceinline__ void piece(const Params& p, float* lds, int b, int ro
       e[j] = __builtin_amdgcn_exp2f(x[j] - m);
       l += e[j];
     }
-    u32x4 pf;
+    u32x4 pf, rest;   // the weights, and what rounding them left
 #pragma unroll
-    for (int w = 0; w < 4; ++w) pf[w] = T::pack(e[2 * w], e[2 * w + 1]);
+    for (int w = 0; w < 4; ++w) {
+      const float e0 = e[2 * w] * kWeight<DT>, e1 = e[2 * w + 1] * kWeight<DT>;
+      pf[w] = T::pack(e0, e1);
+      const f32x2 near = T::unpack(pf[w]);
+      rest[w] = T::pack(e0 - near[0], e1 - near[1]);
+    }
 
     if (edge) {
 #pragma unroll
@@ -333,6 +347,7 @@ __device__ __forceinline__ void piece(const Params& p, float* lds, int b, int ro
         a[w] = __builtin_amdgcn_perm(rows[2 * w + 1][t / 2], rows[2 * w][t / 2],
                                      t % 2 ? 0x07060302u : 0x05040100u);
       acc[t] = T::mfma(a, pf, acc[t]);
+      acc[t] = T::mfma(a, rest, acc[t]);
     }
     if (more) load_v(o0, o1);
   }
