@@ -400,7 +400,9 @@ def fwd_window(q, k, v, window: int, sinks: int = 0, scale: float | None = None,
     visible to every later query.  ``window`` counts the query's own key (at least
     1); a window that reaches every key gives exactly ``fwd(causal=True)``.
     Tensors, types, the other arguments and the results are those of :func:`fwd`
-    (``qm_attn_fwd_window``; key blocks that no query sees cost nothing)."""
+    (``qm_attn_fwd_window``; key blocks that no query sees cost nothing).  As there,
+    every row must be finite, those that pad a batch of prompts among them: a hidden
+    key has probability 0, but 0 times a NaN value is NaN."""
     args, Hkv, N, d, dv, scale, code, out, lse = _checked(q, k, v, scale, out, lse, stream, layout)
     _enqueue(load_library().qm_attn_fwd_window, q.device, stream,
              args + (Hkv, N, d, dv, scale, _int32(window, "window"), _int32(sinks, "sinks")),
