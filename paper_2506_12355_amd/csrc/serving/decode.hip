@@ -42,10 +42,10 @@
 // cuts at most its first row (slot 2 w: a piece that continues a row) and its last
 // (slot 2 w + 1: a piece that begins one).
 //
-// Measured (us; a sum over 1 GiB reads 6.21 TB/s, a floor of 0.161 us a MB): 64 sequences
-// of 0 to 8192 tokens, 64/8 heads, bf16, d = 128 196 (5.5 TB/s), all of 8192 (32 of them)
-// 193 (5.6), of 32768 (64) 1402 (6.13); one of 131072 with E4M3 pages 56 (4.8); one of
-// 1000 9.9, a chain of latencies: length, page numbers, rows, join, second kernel.
+// Measured (us; a sum over 1 GiB reads 6.18 TB/s, a floor of 0.162 us a MB): 64 sequences
+// of 0 to 8192 tokens, 64/8 heads, bf16, d = 128 199 (5.4 TB/s), all of 8192 (32 of them)
+// 195 (5.5), of 32768 (64) 1405 (6.12); one of 131072 with E4M3 pages 58.7 (4.6); one of
+// 1000 10.0, a chain of latencies: length, page numbers, rows, join, second kernel.
 //
 // Window: the blocks walked are those with first keys, then those from the window on;
 // list index i is block i, or i + skip past the first keys' blocks.

@@ -23,7 +23,9 @@ inline int64_t decode_blocks(int64_t limit, int64_t window, int64_t sinks) {
 //
 // A workgroup of eight wavefronts for each row needs no second kernel, but a CU draws
 // about 64 GB/s, and the longest row is waited for.  us, a workgroup a row -> equal
-// shares (bf16, d = 128, rows x tokens, all of one length unless "up to" is said):
+// shares (bf16, d = 128, rows x tokens, all of one length unless "up to" is said; blocks of
+// d = 64 or E4M3, a half or a quarter of the bytes, are divided by the same lines, which
+// were not measured for them):
 // 8 x 300 8.7 -> 9.4, 8 x 1000 14.7 -> 9.9; 32 x 500 10.4 -> 10.7; 64 x 500 11.5 -> 13.4,
 // 64 x 1000 16.0 -> 16.1; 128 x 1000 16.6 -> 19.6, 128 x 2000 37.8 -> 34.9; 256 x 2000
 // 51.7 -> 59.3, 256 x 4000 95.3 -> 104.8; 512 x up to 2000 60.0 -> 63.6, x up to 8192

@@ -16,10 +16,10 @@
 // one stream; several rows in turn, angles and weights kept, were slower (two and four
 // rows a lane, below).
 //
-// Measured (us, bf16, d = 128, a plain copy runs at 5.23 TB/s): 72 heads of 8192 tokens
-// 59.7 (5.1 TB/s; 62.3 and 64.7 with two and four rows a lane), head-major 63.1; one
-// token 3.2 (3.9, 5.9); 4 ragged prompts of up to 2000 tokens into E4M3 pages 33.6
-// (4.4 TB/s), into bf16 ones 35.5.
+// Measured (us, bf16, d = 128, a plain copy runs at 5.24 TB/s): 72 heads of 8192 tokens
+// 58.9 (5.2 TB/s; two and four rows a lane 4% and 8% more), head-major 62.5; one token
+// 3.2 (3.9, 5.9); 4 ragged prompts of up to 2000 tokens into E4M3 pages 29-31
+// (4.7-5.0 TB/s), into bf16 ones 31.7 (5.0).
 #include <type_traits>
 
 #include "serving_device.h"
@@ -48,7 +48,7 @@ struct Params {
   int64_t page_stride;
   int token_stride, head_stride, num_pages, table_cols, fp8;
   FastDiv page;
-  int N, rotary, table_rows, interleaved, bnhd;
+  int rotary, table_rows, interleaved, bnhd;
   float eps;
 };
 
@@ -246,7 +246,7 @@ hipError_t launch(const NormRopeArgs& a, hipStream_t stream) {
   p.token_stride = a.cache.token_stride, p.head_stride = a.cache.head_stride;
   p.num_pages = a.cache.num_pages, p.table_cols = a.cache.table_cols, p.fp8 = a.cache.fp8;
   p.page = FastDiv(a.cache.k ? a.cache.page_size : 1);
-  p.N = a.N, p.rotary = a.rotary, p.table_rows = a.table_rows;
+  p.rotary = a.rotary, p.table_rows = a.table_rows;
   p.interleaved = a.interleaved, p.bnhd = a.layout, p.eps = a.eps;
   hipLaunchKernelGGL((norm_rope_kernel<DT, D>), dim3((units + 3) / 4), dim3(256), 0, stream, p);
   return hipGetLastError();

@@ -48,8 +48,10 @@ struct Type16<1> {
   }
 };
 
-// Exact division of n < 2^31 by a constant of the launch (n d^-1 as a product with
-// the rounded-up reciprocal, its 33rd bit added apart).
+// Exact division of n < 2^31 by a constant of the launch: n d^-1 as a product with the
+// rounded-up reciprocal, its 33rd bit added apart (the method of Granlund and Montgomery,
+// "Division by invariant integers using multiplication", 1994; n + the product's high half
+// fits 32 bits here, so their halving before the sum is not needed).
 struct FastDiv {
   uint32_t d, mul, shift;
   FastDiv() = default;
