@@ -430,7 +430,10 @@ enum LayoutSet : int { kBhndOnly = 0, kEitherLayout = 1, kBnhdOnly = 2 };
 // or j < sinks).  The key loop then walks the blocks that some row of the tile sees, in
 // the order of window_order.h.  A row may see nothing in a step; it keeps m, l and O
 // through it (a masked score's probability is 2^-inf = 0 against any m, -FLT_MAX among
-// them).  Against a walk in ascending order: window 512 4-5%, 1024 2%, 4096 -1%.
+// them).  Time of this order against an instance with an ascending one alone (d = 128, 64,
+// 192): window 512 0.96-0.97, 1024 0.96-0.99, 2048 0.99-1.00, 4096 and 8192 1.00-1.01.
+// One that takes ascending order beyond window 2560 at run time is no faster there
+// (0.99-1.005): what those windows lose is the order's code, so they keep one order.
 template <int DK, int DV, int DT, bool CAUSAL, int WAVES, int G, int LAYOUTS, bool WINDOW = false>
 __device__ __forceinline__ void attn_fwd_body(const KParams& p) {
   using OP = Ops<DT>;

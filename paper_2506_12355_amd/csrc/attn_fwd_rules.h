@@ -45,6 +45,19 @@ inline int key_groups(const AttnArgs& a, int cus) {
   return 1;
 }
 
+// A 256-row tile takes its CU 20 units of time, two 128-row tiles side by side 21, a
+// 128-row tile that has a CU to itself 14: the time of n tiles in whole rounds over the
+// CUs, and of the tiles past the last of them.
+struct Rounds {
+  long long whole, last;
+  Rounds(long long n, int cus, int rows) {
+    const int alone = rows == 256 ? 20 : 14, beside = rows == 256 ? 40 : 21;   // two on a CU
+    const long long left = n % cus, full = n / cus;
+    whole = full / 2 * beside + full % 2 * alone;
+    last = left == 0 ? 0 : full % 2 ? beside - alone : alone;
+  }
+};
+
 // Eight waves keep K/V tiles in LDS for the most rows; four let one workgroup's
 // prologue and epilogue run beside another's key loop, which wins where
 // workgroups are short, and where the 256-row tiles, dealt out in rounds over
@@ -67,10 +80,9 @@ inline int choose_waves(const AttnArgs& a, int cus) {
   // 247 -> 247; d = 64 N = 2048 146 -> 138, N = 4096 274 -> 267, causal
   // 156 -> 150; FP8 N = 4096 282 -> 280, causal 165 -> 161.
   if (a.N <= (a.d == 64 || a.dtype == 2 ? 4096 : a.causal ? 2048 : 1024)) return 4;
-  // Longer ones: a 256-row tile takes its CU 20 units of time, two 128-row
-  // tiles side by side 21, a 128-row tile that has a CU to itself 14.  (B=3 H=32
+  // Longer ones by the time of their rounds (B=3 H=32
   // N=3000: 392 -> 375 us, causal 257 -> 233; B=1 H=24 N=4096 causal, whose
-  // 192 tiles of 256 rows fill 192 CUs: 104 us with them, 109 with 384 halves.)
+  // 192 tiles of 256 rows fill 192 CUs: 104 us with them, 109 with 384 halves).
   // (Where these costs say 1.05, two 128-row tiles for one of 256, 672 shapes beyond
   // N = 4096 took 0.97-1.16 times as long: in the mean 1.06 at d = 128, 1.09 at d = 64,
   // 1.03 with FP8.)
@@ -82,15 +94,15 @@ inline int choose_waves(const AttnArgs& a, int cus) {
   // 140.1 -> 97.2.  After a round of two 128-row tiles beside one another that holds at
   // d = 64 only, where a third fits beside them: H = 8 N = 16500, 264 and 520 tiles,
   // d = 64 311 -> 299, but d = 128 502 -> 530, FP8 296 -> 311.
-  const auto half_units = [&](int rows, int alone, int beside) {   // beside: two on a CU
+  const auto half_units = [&](int rows) {
     const long long n = tiles(rows), left = n % cus, full = n / cus;
     const bool singles = a.causal && (a.N + rows - 1) / rows % 2 &&
                          (long long)a.B * a.H % kXcds == 0 && left <= kXcds &&
                          (rows == 256 || full % 2 || a.d == 64);
-    const long long last = left == 0 ? 0 : full % 2 ? beside - alone : alone;
-    return 2 * (full / 2 * beside + full % 2 * alone) + (singles ? last : 2 * last);
+    const Rounds t(n, cus, rows);
+    return 2 * t.whole + (singles ? t.last : 2 * t.last);
   };
-  return half_units(128, 14, 21) < half_units(256, 20, 40) ? 4 : 8;
+  return half_units(128) < half_units(256) ? 4 : 8;
 }
 
 // Both choices for a sliding window, whose query blocks stay single and take about as
@@ -117,7 +129,7 @@ inline int window_groups(const AttnArgs& a, int cus) {
 // 512 435 -> 469, 1024 652 -> 685, 2048 1061 -> 1069, N = 16384 window 2500 662 -> 661,
 // 3000 756 -> 747, 4096 963 -> 937; but where 256-row tiles end in a round that leaves
 // CUs idle N = 4096 H = 24 window 2500 114 -> 133, N = 8192 H = 10 window 3000 134 -> 153
-// (the costs of choose_waves).  192-wide keys, one workgroup of either size a CU: H = 16
+// (Rounds).  192-wide keys, one workgroup of either size a CU: H = 16
 // N = 4096 window 512 42.5 -> 38.4, H = 8 (all 128-row tiles at once) 22.3 -> 29.2.
 // d = 64: 128 rows (256 with this kernel before its masks went by halves: N = 8192 B = 4
 // H = 32 window 256 235 -> 350, N = 32768 window 8192 2169 -> 2283).
@@ -125,11 +137,11 @@ inline int choose_window_waves(const AttnArgs& a, int cus) {
   const auto tiles = [&](int rows) { return (long long)((a.N + rows - 1) / rows) * a.B * a.H; };
   if (a.d == 192) return tiles(128) <= cus ? 4 : 8;
   if (a.d == 64 || a.window <= 2560) return 4;
-  const auto units = [&](int rows, int alone, int beside) {
-    const long long left = tiles(rows) % cus, full = tiles(rows) / cus;
-    return full / 2 * beside + full % 2 * alone + (left == 0 ? 0 : full % 2 ? beside - alone : alone);
+  const auto units = [&](int rows) {
+    const Rounds t(tiles(rows), cus, rows);
+    return t.whole + t.last;
   };
-  return units(128, 14, 21) < units(256, 20, 40) ? 4 : 8;
+  return units(128) < units(256) ? 4 : 8;
 }
 
 // Workgroups of a launch over `total` tiles: as many as are `resident` at once, each
