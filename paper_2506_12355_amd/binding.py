@@ -267,8 +267,10 @@ def _pool_of(stream, new):
     that the call runs on.  From the current stream's pool, beside a `stream` of the
     caller's, their memory could still be in use by that stream's earlier work, and be given
     out to its later work while the kernel writes it: nothing orders the two."""
+    if stream is None or not new:
+        return _CURRENT
     import torch
-    return torch.cuda.stream(stream) if new and stream is not None else _CURRENT
+    return torch.cuda.stream(stream)
 
 
 def _lse(q, lse, B, H, N):
