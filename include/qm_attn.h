@@ -378,7 +378,8 @@ int qm_qk_norm_rope(const void* q, const void* k, void* q_out, void* k_out,
  *   stored as they are.
  *   Rows past a sequence's count store nothing.  A token whose position is outside
  *   the rotation's table or the page table, or whose page number is out of range,
- *   is not stored.  Pages that hold a written position must belong to one sequence.
+ *   is not stored.  Pages that hold a written position must belong to one sequence and
+ *   stand once in its row of the table (else either token's bytes may stay there).
  */
 int qm_qk_norm_rope_append(const void* q, const void* k, const void* v, void* q_out, void* k_out,
                            void* k_cache, void* v_cache, const int* page_table,

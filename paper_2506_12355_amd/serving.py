@@ -214,7 +214,8 @@ def qk_norm_rope_append(q, k, v, k_cache, v_cache, page_table, starts=None, cos=
     The cache holds key / ``k_scale`` and value / ``v_scale`` (with E4M3 pages, values
     beyond 448 as 448).  Its pages past a sequence's tokens are left as they were, and so
     are the entries of ``page_table`` that name them.  A token whose position has no page
-    (or no angle, or a page number out of range) is not stored.  v has k's shape and any
+    (or no angle, or a page number out of range) is not stored.  A page that is written
+    belongs to one sequence and stands once in its row.  v has k's shape and any
     strides as q and k; ``k_out``, where given, receives the keys as ``qk_norm_rope``
     returns them.  Without cos, sin and weights the keys are stored as they are.  Returns
     q_out (``qm_qk_norm_rope_append``)."""
