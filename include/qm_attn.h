@@ -99,7 +99,11 @@ enum {
                               (starts NULL) shorter than N, eps is negative, infinite or NaN, or
                               interleaved is neither 0 nor 1 */
   QM_ERR_STRIDE = -15,     /* a stride is negative or not a multiple of 8 elements */
-  QM_ERR_WORKSPACE = -16   /* workspace is NULL or smaller than the call needs */
+  QM_ERR_WORKSPACE = -16,  /* workspace is NULL or smaller than the call needs */
+  QM_ERR_NORM = -17,       /* qm_rms_norm: width is not a multiple of 8 from 8 to 32768 (and of
+                              group, which is 0, 32, 64, 128 or 256), or eps not finite or below 0 */
+  QM_ERR_AXES = -18        /* positions of several axes: axes not from 1 to 4, a pair's axis not
+                              below axes, or starts given to a call that writes no cache */
 };
 
 /*
@@ -391,6 +395,83 @@ int qm_qk_norm_rope_append(const void* q, const void* k, const void* v, void* q_
                            const long long* k_strides, const long long* v_strides,
                            hipStream_t stream, int dtype, int layout, int cache_dtype,
                            int cache_layout);
+
+/*
+ * qm_qk_norm_rope_axes, qm_qk_norm_rope_append_axes - the two calls above with positions of
+ * several axes (time, height and width of a picture's parts, say): pair j of token t of
+ * sequence b turns by row positions[pair_axis[j]][b][t] of the table's column j.
+ *
+ *   positions    [in]  device, [axes][B][N] int32, 4-byte aligned.  Places past a sequence's
+ *                      count, and axes that no pair has, are not looked at.
+ *   axes         1 to 4.
+ *   pair_axis    [in]  host, [rotary / 2] bytes, each below axes, read during the call.
+ *   rotary       above 0.
+ *   starts       qm_qk_norm_rope_axes: no such argument, the positions stand for it.
+ *                qm_qk_norm_rope_append_axes: a token's place in the cache alone, starts[b] + t.
+ *   A token with a position outside the table on an axis that some pair has gets NaN rows
+ *   and is not stored.  Everything else is as above.
+ */
+int qm_qk_norm_rope_axes(const void* q, const void* k, void* q_out, void* k_out,
+                         const void* q_weight, const void* k_weight, const float* cos,
+                         const float* sin, const int* positions, const unsigned char* pair_axis,
+                         int axes, const int* counts, int B, int H, int Hkv, int N, int d,
+                         int rotary, int table_rows, float eps, int interleaved,
+                         const long long* q_strides, const long long* k_strides,
+                         hipStream_t stream, int dtype, int layout);
+
+int qm_qk_norm_rope_append_axes(
+    const void* q, const void* k, const void* v, void* q_out, void* k_out, void* k_cache,
+    void* v_cache, const int* page_table, const void* q_weight, const void* k_weight,
+    const float* cos, const float* sin, const int* positions, const unsigned char* pair_axis,
+    int axes, const int* starts, const int* counts, int B, int H, int Hkv, int N, int d, int rotary,
+    int table_rows, float eps, int interleaved, int num_pages, int page_size, int table_cols,
+    float k_scale, float v_scale, const long long* q_strides, const long long* k_strides,
+    const long long* v_strides, hipStream_t stream, int dtype, int layout, int cache_dtype,
+    int cache_layout);
+
+/*
+ * qm_rms_norm - the residual's addition and the norm of whole rows, between two layers.
+ * Per row x of `width` columns and r of the residual (where it is given, else 0):
+ *
+ *   s_c = x_c + r_c,      y_c = s_c w_c / sqrt(mean(s^2) + eps)     (w = 1 without a weight)
+ *
+ * in fp32; s is rounded into `sum`, and y, of the s that is not rounded, into `out`.
+ *
+ *   x, residual  [in]  device, [rows][width] of `dtype`; x_stride and residual_stride are the
+ *                      elements from row to row: multiples of 8, 0 or more (of a single row
+ *                      not looked at); a row's columns are contiguous.  residual may be NULL.
+ *   weight       [in]  device, [width] of `dtype`, or NULL.
+ *   out          [out] device, contiguous [rows][width] of `dtype`.  Overlaps nothing.
+ *   sum          [out] device, [rows][width] of `dtype` with sum_stride elements, `width` or
+ *                      more, from row to row; NULL: not written.  It may be x or the residual
+ *                      itself, with the same stride, and overlaps nothing else.  Given with
+ *                      a residual only (QM_ERR_NULL).
+ *   width        a multiple of 8 from 8 to 32768 (QM_ERR_NORM).     rows   1 or more.
+ *   A row whose mean square overflows fp32 has y = 0; one that holds a NaN or an infinity
+ *   has NaN in y, there at least.  Other rows are not affected.
+ *   stream, errors, capture: as for the calls above (one kernel, nothing else).
+ */
+int qm_rms_norm(const void* x, const void* residual, const void* weight, void* out, void* sum,
+                int rows, int width, long long x_stride, long long residual_stride,
+                long long sum_stride, float eps, hipStream_t stream, int dtype);
+
+/*
+ * qm_rms_norm_fp8 - qm_rms_norm with E4M3 codes of y / scale in `out` ([rows][width] bytes;
+ * the quotient as a product with the fp32 reciprocal, to nearest even; beyond 448, 448; NaN
+ * stays NaN).
+ *
+ *   scales       [out] device, fp32, 4-byte aligned: [rows][width / group], or [rows] for
+ *                      group = 0.  Each is max |y| / 448 over its columns, at least 2^-126
+ *                      (NaN if a y is).  NULL: `scale` is every column's, and nothing is written.
+ *   group        columns of a scale: 32, 64, 128, 256, or 0 for the row (QM_ERR_NORM; 0
+ *                      without scales).  width is a multiple of it.
+ *   scale        without scales: finite, above 0, with a finite reciprocal (QM_ERR_SCALE).
+ *                      With scales it is not looked at.
+ */
+int qm_rms_norm_fp8(const void* x, const void* residual, const void* weight, void* out,
+                    float* scales, void* sum, int rows, int width, long long x_stride,
+                    long long residual_stride, long long sum_stride, float eps, float scale,
+                    int group, hipStream_t stream, int dtype);
 
 /*
  * qm_attn_decode - attention of one new token per sequence over the cache.  Query

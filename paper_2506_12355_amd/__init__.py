@@ -18,11 +18,13 @@ from .binding import (  # noqa: F401
     QM_BHND,
     QM_BNHD,
     QM_ERR_ALIAS,
+    QM_ERR_AXES,
     QM_ERR_CAUSAL,
     QM_ERR_DTYPE,
     QM_ERR_HEADDIM,
     QM_ERR_LAUNCH,
     QM_ERR_LAYOUT,
+    QM_ERR_NORM,
     QM_ERR_NULL,
     QM_ERR_PAGE,
     QM_ERR_ROTARY,
@@ -57,4 +59,6 @@ from .serving import (  # noqa: F401
     decode_workspace,
     qk_norm_rope,
     qk_norm_rope_append,
+    rms_norm,
+    rms_norm_fp8,
 )

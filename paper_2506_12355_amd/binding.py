@@ -42,6 +42,8 @@ QM_ERR_PAGE = -13
 QM_ERR_ROTARY = -14
 QM_ERR_STRIDE = -15
 QM_ERR_WORKSPACE = -16
+QM_ERR_NORM = -17
+QM_ERR_AXES = -18
 
 _lib = None
 _lock = threading.Lock()
@@ -107,6 +109,17 @@ def _declare(lib: ctypes.CDLL) -> ctypes.CDLL:
     lib.qm_qk_norm_rope_append.argtypes = (
         [P] * 14 + [I] * 7 + [F] + [I] * 4 + [F] * 2 + [P] * 4 + [I] * 4)
     lib.qm_qk_norm_rope_append.restype = ctypes.c_int
+    lib.qm_qk_norm_rope_axes.argtypes = (
+        [P] * 10 + [I, P] + [I] * 7 + [F, I] + [P] * 3 + [I] * 2)
+    lib.qm_qk_norm_rope_axes.restype = ctypes.c_int
+    lib.qm_qk_norm_rope_append_axes.argtypes = (
+        [P] * 14 + [I] + [P] * 2 + [I] * 7 + [F] + [I] * 4 + [F] * 2 + [P] * 4 + [I] * 4)
+    lib.qm_qk_norm_rope_append_axes.restype = ctypes.c_int
+    L = ctypes.c_longlong
+    lib.qm_rms_norm.argtypes = [P] * 5 + [I] * 2 + [L] * 3 + [F, P, I]
+    lib.qm_rms_norm.restype = ctypes.c_int
+    lib.qm_rms_norm_fp8.argtypes = [P] * 6 + [I] * 2 + [L] * 3 + [F] * 2 + [I, P, I]
+    lib.qm_rms_norm_fp8.restype = ctypes.c_int
     lib.qm_attn_decode.argtypes = (
         [P] * 7 + [I] * 8 + [F] * 3 + [I] * 2 + [P, ctypes.c_size_t, P] + [I] * 3)
     lib.qm_attn_decode.restype = ctypes.c_int
@@ -304,13 +317,13 @@ def _enqueue(entry, device, stream, before, after) -> None:
         raise QmAttnError(status, strerror(status))
 
 
-def _dtype_code(t) -> int:
+def _dtype_code(t, name: str = "q, k, v") -> int:
     import torch
     if t.dtype == torch.float16:
         return QM_F16
     if t.dtype == torch.bfloat16:
         return QM_BF16
-    raise TypeError(f"q, k, v must be float16 or bfloat16, not {t.dtype}")
+    raise TypeError(f"{name} must be float16 or bfloat16, not {t.dtype}")
 
 
 def _checked(q, k, v, scale, out, lse, stream, layout):

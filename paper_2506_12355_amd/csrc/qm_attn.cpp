@@ -209,6 +209,10 @@ extern "C" const char* qm_attn_strerror(int status) {
              "positions, eps finite and not negative, interleaved 0 or 1";
     case QM_ERR_STRIDE: return "strides must be multiples of 8 elements and not negative";
     case QM_ERR_WORKSPACE: return "the workspace is smaller than the call needs";
+    case QM_ERR_NORM:
+      return "a row's width must be a multiple of 8 from 8 to 32768 and of its scales' group (32, 64, "
+             "128, 256 or the row), and eps finite and not negative";
+    case QM_ERR_AXES: return "1 to 4 axes with positions, and an axis for each rotated pair";
   }
   return "unknown status";
 }

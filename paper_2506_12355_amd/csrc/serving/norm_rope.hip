@@ -20,8 +20,6 @@
 // 58.9 (5.2 TB/s; two and four rows a lane 4% and 8% more), head-major 62.5; one token
 // 3.2 (3.9, 5.9); 4 ragged prompts of up to 2000 tokens into E4M3 pages 29-31
 // (4.7-5.0 TB/s), into bf16 ones 31.7 (5.0).
-#include <type_traits>
-
 #include "serving_device.h"
 #include "serving_launch.h"
 
@@ -50,6 +48,11 @@ struct Params {
   FastDiv page;
   int rotary, table_rows, interleaved, bnhd;
   float eps;
+  // positions of several axes
+  const int32_t* positions;
+  int64_t axis_stride;
+  int N, used_axes;
+  uint64_t pair_axis[2];
 };
 
 // Sum over the L (4 or 8) neighbouring lanes that hold a row.
@@ -65,17 +68,8 @@ __device__ __forceinline__ float row_sum(float x) {
   return x;
 }
 
-// To E4M3, to nearest even, beyond +-448 the largest value; NaN stays NaN.
-__device__ __forceinline__ float to_range(float x) {
-  return x != x ? x : fminf(fmaxf(x, -448.f), 448.f);
-}
-__device__ __forceinline__ uint32_t pack_fp8(float a, float b, float c, float d) {
-  int w = __builtin_amdgcn_cvt_pk_fp8_f32(to_range(a), to_range(b), 0, false);
-  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(to_range(c), to_range(d), w, true);
-}
-
 // The rows of one unit of q (KIND 0), k (1) or v (2).
-template <int DT, int D, int KIND>
+template <int DT, int D, bool AXES, int KIND>
 __device__ __forceinline__ void unit_rows(const Params& p, const Stream& s, uint32_t unit) {
   using T = Type16<DT>;
   constexpr int L = D / 16;      // lanes of a row
@@ -111,7 +105,17 @@ __device__ __forceinline__ void unit_rows(const Params& p, const Stream& s, uint
   }
   const int64_t at = (int64_t)(p.starts ? p.starts[b] : 0) + t;
   const bool held = !p.counts || (int)t < p.counts[b];
-  const bool fits = !p.rotary || (at >= 0 && at < p.table_rows);
+  bool fits = !p.rotary || (at >= 0 && at < p.table_rows);
+  int row0 = 0, row1 = 0, row2 = 0, row3 = 0;   // the token's row of the table on each axis
+  if (AXES && held) {
+    const int32_t* own = p.positions + (int64_t)b * p.N + t;
+    if (p.used_axes & 1) row0 = own[0];
+    if (p.used_axes & 2) row1 = own[p.axis_stride];
+    if (p.used_axes & 4) row2 = own[2 * p.axis_stride];
+    if (p.used_axes & 8) row3 = own[3 * p.axis_stride];
+    auto inside = [&](int r) __attribute__((always_inline)) { return (uint32_t)r < (uint32_t)p.table_rows; };
+    fits = inside(row0) && inside(row1) && inside(row2) && inside(row3);
+  }
 
   float x[8], y[8];
   if (held) {
@@ -137,13 +141,35 @@ __device__ __forceinline__ void unit_rows(const Params& p, const Stream& s, uint
       }
     }
     if (turned && fits) {
-      const float* ct = p.cos + at * half + 8 * i;
-      const float* st = p.sin + at * half + 8 * i;
       f32x4 cv[2], sv[2];
+      int64_t line = at;
+      bool one = true;   // the lane's pairs lie in one row of the table
+      if (AXES) {
+        // the axes of pairs 8 i .. 8 i + 7
+        const uint32_t of = (uint32_t)(p.pair_axis[i >= 4] >> (16 * (i & 3))) & 0xffffu;
+        auto row_of = [&](uint32_t a) __attribute__((always_inline)) {
+          const int low = a & 1 ? row1 : row0, high = a & 1 ? row3 : row2;
+          return a & 2 ? high : low;
+        };
+        line = row_of(of & 3);
+        one = of == (of & 3) * 0x5555u;
+        if (!one) {
 #pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        cv[j] = reinterpret_cast<const f32x4*>(ct)[j];
-        sv[j] = reinterpret_cast<const f32x4*>(st)[j];
+          for (int j = 0; j < 8; ++j) {
+            const int64_t from = (int64_t)row_of(of >> (2 * j) & 3) * half + 8 * i + j;
+            cv[j / 4][j % 4] = p.cos[from];
+            sv[j / 4][j % 4] = p.sin[from];
+          }
+        }
+      }
+      if (one) {
+        const float* ct = p.cos + line * half + 8 * i;
+        const float* st = p.sin + line * half + 8 * i;
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          cv[j] = reinterpret_cast<const f32x4*>(ct)[j];
+          sv[j] = reinterpret_cast<const f32x4*>(st)[j];
+        }
       }
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
@@ -206,14 +232,14 @@ __device__ __forceinline__ void unit_rows(const Params& p, const Stream& s, uint
   }
 }
 
-template <int DT, int D>
+template <int DT, int D, bool AXES>
 __global__ __launch_bounds__(256) void norm_rope_kernel(Params p) {
   uint32_t unit = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
-  if (unit < p.s[0].units) return unit_rows<DT, D, 0>(p, p.s[0], unit);
+  if (unit < p.s[0].units) return unit_rows<DT, D, AXES, 0>(p, p.s[0], unit);
   unit -= p.s[0].units;
-  if (unit < p.s[1].units) return unit_rows<DT, D, 1>(p, p.s[1], unit);
+  if (unit < p.s[1].units) return unit_rows<DT, D, AXES, 1>(p, p.s[1], unit);
   unit -= p.s[1].units;
-  if (unit < p.s[2].units) unit_rows<DT, D, 2>(p, p.s[2], unit);
+  if (unit < p.s[2].units) unit_rows<DT, D, AXES, 2>(p, p.s[2], unit);
 }
 
 template <int DT, int D>
@@ -248,7 +274,15 @@ hipError_t launch(const NormRopeArgs& a, hipStream_t stream) {
   p.page = FastDiv(a.cache.k ? a.cache.page_size : 1);
   p.rotary = a.rotary, p.table_rows = a.table_rows;
   p.interleaved = a.interleaved, p.bnhd = a.layout, p.eps = a.eps;
-  hipLaunchKernelGGL((norm_rope_kernel<DT, D>), dim3((units + 3) / 4), dim3(256), 0, stream, p);
+  if (a.positions) {
+    p.positions = a.positions;
+    p.axis_stride = (int64_t)a.B * a.N;
+    p.N = a.N, p.used_axes = a.used_axes;
+    p.pair_axis[0] = a.pair_axis[0], p.pair_axis[1] = a.pair_axis[1];
+    hipLaunchKernelGGL((norm_rope_kernel<DT, D, true>), dim3((units + 3) / 4), dim3(256), 0, stream, p);
+    return hipGetLastError();
+  }
+  hipLaunchKernelGGL((norm_rope_kernel<DT, D, false>), dim3((units + 3) / 4), dim3(256), 0, stream, p);
   return hipGetLastError();
 }
 

@@ -97,7 +97,14 @@ bool reciprocal(float scale, float* inv) {
   return finite_bits(scale) && scale != 0.0f && finite_bits(*inv) && *inv != 0.0f;
 }
 
-// Both entry points; cached: the one that writes a cache.
+// The positions of several axes (NULL where a call has none).
+struct Axes {
+  const int* positions;
+  const unsigned char* pair_axis;
+  int count;
+};
+
+// All four entry points; cached: those that write a cache.
 int norm_rope(const void* q, const void* k, const void* v, void* q_out, void* k_out, void* k_cache,
               void* v_cache, const int* page_table, const void* q_weight, const void* k_weight,
               const float* cos, const float* sin, const int* starts, const int* counts, int B, int H,
@@ -105,10 +112,11 @@ int norm_rope(const void* q, const void* k, const void* v, void* q_out, void* k_
               int num_pages, int page_size, int table_cols, float k_scale, float v_scale,
               const long long* q_strides, const long long* k_strides, const long long* v_strides,
               hipStream_t stream, int dtype, int layout, int cache_dtype, int cache_layout,
-              bool cached) {
+              bool cached, const Axes* axes) {
   if (!q || !k || !q_out) return QM_ERR_NULL;
   if (cached ? !v || !k_cache || !v_cache || !page_table : !k_out) return QM_ERR_NULL;
   if (rotary > 0 && (!cos || !sin)) return QM_ERR_NULL;
+  if (axes && (!axes->positions || !axes->pair_axis)) return QM_ERR_NULL;
   if (B < 1 || H < 1 || Hkv < 1 || N < 1) return QM_ERR_SHAPE;
   if (d != 64 && d != 128) return QM_ERR_HEADDIM;
   // rows in all: the launch's threads (d / 16 a row, rounded up to wavefronts) fit 31 bits
@@ -120,9 +128,20 @@ int norm_rope(const void* q, const void* k, const void* v, void* q_out, void* k_
   if (rotary < 0 || rotary > d || rotary % 16 || (interleaved != 0 && interleaved != 1) ||
       !finite_bits(eps) || eps < 0.0f)
     return QM_ERR_ROTARY;
-  if (rotary > 0 && (table_rows < 1 || (!starts && N > table_rows))) return QM_ERR_ROTARY;
+  if (rotary > 0 && (table_rows < 1 || (!axes && !starts && N > table_rows))) return QM_ERR_ROTARY;
 
   qm::NormRopeArgs a = {};
+  if (axes) {
+    if (rotary == 0) return QM_ERR_ROTARY;
+    if (axes->count < 1 || axes->count > 4) return QM_ERR_AXES;
+    for (int j = 0; j < rotary / 2; ++j) {
+      const uint64_t axis = axes->pair_axis[j];
+      if (axis >= (uint64_t)axes->count) return QM_ERR_AXES;
+      a.pair_axis[j / 32] |= axis << (2 * (j % 32));
+      a.used_axes |= 1 << axis;
+    }
+    a.positions = axes->positions;
+  }
   uint64_t cache_bytes = 0;
   if (cached) {
     const int st = check_cache(&a.cache, &cache_bytes, Hkv, d, num_pages, page_size, table_cols,
@@ -144,7 +163,8 @@ int norm_rope(const void* q, const void* k, const void* v, void* q_out, void* k_
                       {q_weight, (uint64_t)d * 2}, {k_weight, (uint64_t)d * 2},
                       {table ? cos : nullptr, table}, {table ? sin : nullptr, table},
                       {starts, (uint64_t)B * 4}, {counts, (uint64_t)B * 4},
-                      {cached ? page_table : nullptr, (uint64_t)B * (uint64_t)(cached ? table_cols : 0) * 4}};
+                      {cached ? page_table : nullptr, (uint64_t)B * (uint64_t)(cached ? table_cols : 0) * 4},
+                      {a.positions, axes ? (uint64_t)axes->count * (uint64_t)B * (uint64_t)N * 4 : 0}};
   const uint64_t row_bytes = (uint64_t)B * N * d * 2;
   const Range out[] = {{q_out, row_bytes * H}, {k_out, row_bytes * Hkv},
                        {cached ? k_cache : nullptr, cache_bytes}, {cached ? v_cache : nullptr, cache_bytes}};
@@ -156,7 +176,7 @@ int norm_rope(const void* q, const void* k, const void* v, void* q_out, void* k_
   }
   for (int i = 0; i < 7; ++i)
     if (in[i].p && !aligned16(in[i].p)) return QM_ERR_UNSUPPORTED;
-  for (int i = 7; i < 10; ++i)
+  for (int i = 7; i < 11; ++i)
     if (in[i].p && !aligned4(in[i].p)) return QM_ERR_UNSUPPORTED;
   for (const Range& r : out)
     if (r.p && !aligned16(r.p)) return QM_ERR_UNSUPPORTED;
@@ -184,6 +204,65 @@ int norm_rope(const void* q, const void* k, const void* v, void* q_out, void* k_
   a.layout = layout;
   a.eps = eps;
   return qm::launch_norm_rope(a, stream) == hipSuccess ? QM_OK : QM_ERR_LAUNCH;
+}
+
+// Bytes from a tensor's first row to the end of its last.
+uint64_t rows_span(int rows, int width, int64_t stride) {
+  return (times((uint64_t)(rows - 1), (uint64_t)stride) + (uint64_t)width) * 2;
+}
+
+// Both entry points; fp8: the one of E4M3 codes.
+int rms_norm(const void* x, const void* residual, const void* weight, void* out, float* scales,
+             void* sum, int rows, int width, long long x_stride, long long residual_stride,
+             long long sum_stride, float eps, float scale, int group, hipStream_t stream, int dtype,
+             bool fp8) {
+  if (!x || !out || (sum && !residual)) return QM_ERR_NULL;
+  if (rows < 1) return QM_ERR_SHAPE;
+  if (dtype != QM_F16 && dtype != QM_BF16) return QM_ERR_DTYPE;
+  if (width < 8 || width > 32768 || width % 8 || !finite_bits(eps) || eps < 0.0f) return QM_ERR_NORM;
+  if (group && (!scales || (group != 32 && group != 64 && group != 128 && group != 256) || width % group))
+    return QM_ERR_NORM;
+  qm::RmsNormArgs a = {};
+  if (fp8 && !scales && (!(scale > 0.0f) || !reciprocal(scale, &a.inv))) return QM_ERR_SCALE;
+  a.x_stride = rows == 1 ? width : x_stride;
+  a.residual_stride = rows == 1 || !residual ? width : residual_stride;
+  a.sum_stride = rows == 1 || !sum ? width : sum_stride;
+  if (a.x_stride < 0 || a.x_stride % 8 || a.residual_stride < 0 || a.residual_stride % 8 ||
+      a.sum_stride < width || a.sum_stride % 8)
+    return QM_ERR_STRIDE;
+  const uint64_t spans[3] = {rows_span(rows, width, a.x_stride), rows_span(rows, width, a.residual_stride),
+                             rows_span(rows, width, a.sum_stride)};
+  for (uint64_t s : spans)
+    if (s >= kMost / 4) return QM_ERR_SHAPE;
+  const uint64_t elements = (uint64_t)rows * (uint64_t)width;   // below 2^46
+  const Range rx = {x, spans[0]}, rr = {residual, spans[1]}, rw = {weight, (uint64_t)width * 2};
+  const Range ro = {out, elements * (fp8 ? 1 : 2)}, rs = {sum, spans[2]};
+  const Range rc = {scales, elements / (uint64_t)(group ? group : width) * 4};
+  const Range in[] = {rx, rr, rw}, others[] = {rw, ro, rc};
+  if (any_overlap(ro, in) || any_overlap(rc, in) || any_overlap(rs, others)) return QM_ERR_ALIAS;
+  const Range codes[] = {ro};
+  if (any_overlap(rc, codes)) return QM_ERR_ALIAS;
+  // the sum may take the place of x or of the residual, whose rows its threads hold by then
+  const bool is_x = sum == x && a.sum_stride == a.x_stride;
+  const bool is_residual = sum == residual && a.sum_stride == a.residual_stride;
+  const Range first[] = {rx}, second[] = {rr};
+  if ((!is_x && any_overlap(rs, first)) || (!is_residual && any_overlap(rs, second))) return QM_ERR_ALIAS;
+  if (!aligned16(x) || !aligned16(residual) || !aligned16(weight) || !aligned16(out) ||
+      !aligned16(sum) || !aligned4(scales))
+    return QM_ERR_UNSUPPORTED;
+  a.x = static_cast<const uint16_t*>(x);
+  a.residual = static_cast<const uint16_t*>(residual);
+  a.weight = static_cast<const uint16_t*>(weight);
+  a.sum = static_cast<uint16_t*>(sum);
+  a.out = out;
+  a.scales = scales;
+  a.rows = rows;
+  a.width = width;
+  a.group = group;
+  a.fp8 = fp8;
+  a.dtype = dtype;
+  a.eps = eps;
+  return qm::launch_rms_norm(a, stream) == hipSuccess ? QM_OK : QM_ERR_LAUNCH;
 }
 
 // CUs of the current device (asked once for each of the first 64), or 0.
@@ -236,7 +315,7 @@ extern "C" int qm_qk_norm_rope(const void* q, const void* k, void* q_out, void* 
                                int layout) {
   return norm_rope(q, k, nullptr, q_out, k_out, nullptr, nullptr, nullptr, q_weight, k_weight, cos,
                    sin, starts, counts, B, H, Hkv, N, d, rotary, table_rows, eps, interleaved, 0, 0,
-                   0, 1.0f, 1.0f, q_strides, k_strides, nullptr, stream, dtype, layout, 0, 0, false);
+                   0, 1.0f, 1.0f, q_strides, k_strides, nullptr, stream, dtype, layout, 0, 0, false, nullptr);
 }
 
 extern "C" int qm_qk_norm_rope_append(
@@ -250,7 +329,54 @@ extern "C" int qm_qk_norm_rope_append(
   return norm_rope(q, k, v, q_out, k_out, k_cache, v_cache, page_table, q_weight, k_weight, cos, sin,
                    starts, counts, B, H, Hkv, N, d, rotary, table_rows, eps, interleaved, num_pages,
                    page_size, table_cols, k_scale, v_scale, q_strides, k_strides, v_strides, stream,
-                   dtype, layout, cache_dtype, cache_layout, true);
+                   dtype, layout, cache_dtype, cache_layout, true, nullptr);
+}
+
+extern "C" int qm_qk_norm_rope_axes(const void* q, const void* k, void* q_out, void* k_out,
+                                    const void* q_weight, const void* k_weight, const float* cos,
+                                    const float* sin, const int* positions,
+                                    const unsigned char* pair_axis, int axes, const int* counts, int B,
+                                    int H, int Hkv, int N, int d, int rotary, int table_rows, float eps,
+                                    int interleaved, const long long* q_strides,
+                                    const long long* k_strides, hipStream_t stream, int dtype,
+                                    int layout) {
+  const Axes given = {positions, pair_axis, axes};
+  return norm_rope(q, k, nullptr, q_out, k_out, nullptr, nullptr, nullptr, q_weight, k_weight, cos,
+                   sin, nullptr, counts, B, H, Hkv, N, d, rotary, table_rows, eps, interleaved, 0, 0,
+                   0, 1.0f, 1.0f, q_strides, k_strides, nullptr, stream, dtype, layout, 0, 0, false,
+                   &given);
+}
+
+extern "C" int qm_qk_norm_rope_append_axes(
+    const void* q, const void* k, const void* v, void* q_out, void* k_out, void* k_cache,
+    void* v_cache, const int* page_table, const void* q_weight, const void* k_weight,
+    const float* cos, const float* sin, const int* positions, const unsigned char* pair_axis,
+    int axes, const int* starts, const int* counts, int B, int H, int Hkv, int N, int d, int rotary,
+    int table_rows, float eps, int interleaved, int num_pages, int page_size, int table_cols,
+    float k_scale, float v_scale, const long long* q_strides, const long long* k_strides,
+    const long long* v_strides, hipStream_t stream, int dtype, int layout, int cache_dtype,
+    int cache_layout) {
+  const Axes given = {positions, pair_axis, axes};
+  return norm_rope(q, k, v, q_out, k_out, k_cache, v_cache, page_table, q_weight, k_weight, cos, sin,
+                   starts, counts, B, H, Hkv, N, d, rotary, table_rows, eps, interleaved, num_pages,
+                   page_size, table_cols, k_scale, v_scale, q_strides, k_strides, v_strides, stream,
+                   dtype, layout, cache_dtype, cache_layout, true, &given);
+}
+
+extern "C" int qm_rms_norm(const void* x, const void* residual, const void* weight, void* out,
+                           void* sum, int rows, int width, long long x_stride,
+                           long long residual_stride, long long sum_stride, float eps,
+                           hipStream_t stream, int dtype) {
+  return rms_norm(x, residual, weight, out, nullptr, sum, rows, width, x_stride, residual_stride,
+                  sum_stride, eps, 1.0f, 0, stream, dtype, false);
+}
+
+extern "C" int qm_rms_norm_fp8(const void* x, const void* residual, const void* weight, void* out,
+                               float* scales, void* sum, int rows, int width, long long x_stride,
+                               long long residual_stride, long long sum_stride, float eps,
+                               float scale, int group, hipStream_t stream, int dtype) {
+  return rms_norm(x, residual, weight, out, scales, sum, rows, width, x_stride, residual_stride,
+                  sum_stride, eps, scale, group, stream, dtype, true);
 }
 
 extern "C" int qm_attn_decode_workspace(int B, int H, int Hkv, int d, int page_size, int table_cols,

@@ -27,11 +27,26 @@ struct NormRopeArgs {
   int64_t stride[3][3];                  // q, k, v: elements from batch to batch, token, head
   int B, H, Hkv, N, d, rotary, table_rows, interleaved, dtype, layout;
   float eps;
+  const int32_t* positions;              // [axes][B][N], or NULL: starts + t
+  int used_axes;                         // bit a set where a pair has axis a
+  uint64_t pair_axis[2];                 // the axis of pair j: bits 2 (j % 32) .. of word j / 32
   float k_inv, v_inv;                    // what cached keys and values are multiplied by
   PagedCache cache;                      // cache.k NULL: none
 };
 
 hipError_t launch_norm_rope(const NormRopeArgs& a, hipStream_t stream);
+
+struct RmsNormArgs {
+  const uint16_t *x, *residual, *weight;   // residual and weight may be NULL
+  uint16_t* sum;                           // x + residual, or NULL
+  void* out;                               // [rows][width], 16 bits or E4M3
+  float* scales;                           // [rows][width / group], or [rows]; NULL: `inv` for all
+  int64_t x_stride, residual_stride, sum_stride;   // elements from row to row
+  int rows, width, group, fp8, dtype;      // group 0: a scale a row
+  float eps, inv;
+};
+
+hipError_t launch_rms_norm(const RmsNormArgs& a, hipStream_t stream);
 
 struct DecodeArgs {
   const uint16_t* q;       // [B][H][d]

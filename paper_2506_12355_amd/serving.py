@@ -14,6 +14,7 @@ from __future__ import annotations
 
 import ctypes
 import functools
+import operator
 
 from .binding import (QM_BHND, QM_BNHD, QM_OK, QmAttnError, _dtype_code, _enqueue, _int32,
                       _pool_of, load_library, strerror)
@@ -158,9 +159,33 @@ def _cache(k_cache, v_cache, page_table, B, d, dtype, code, index, cache_layout)
     return pages, page_size, heads, columns[1], table, code, layout
 
 
+@functools.lru_cache(maxsize=64)
+def _pair_axes(axes, pairs, count):
+    """The library's array of each pair's axis."""
+    if axes is None:
+        if count != 1:
+            raise ValueError("axes must name each rotated pair's axis where positions has several")
+        return bytes(pairs)
+    if len(axes) != pairs:
+        raise ValueError(f"axes must name the axis of each of the {pairs} rotated pairs, not of {len(axes)}")
+    axes = [operator.index(a) for a in axes]
+    if not all(0 <= a < count for a in axes):
+        raise ValueError(f"axes must be from 0 to {count - 1}, positions' axes")
+    return bytes(axes)
+
+
+def _positions(positions, axes, rotary, B, N, index):
+    """The library's arguments for positions of several axes: addresses, and their number."""
+    size = positions.shape
+    if len(size) != 3 or not 1 <= size[0] <= 4:
+        raise ValueError("positions must have shape [axes, B, N] with 1 to 4 axes")
+    at = _vector("positions", positions, (size[0], B, N), index, _torch().int32)
+    return at, _pair_axes(axes if axes is None else tuple(axes), rotary // 2, size[0]), size[0]
+
+
 def qk_norm_rope(q, k, cos=None, sin=None, q_weight=None, k_weight=None, eps: float = 1e-6,
                  starts=None, counts=None, interleaved: bool = False, q_out=None, k_out=None,
-                 stream=None, layout: str = "bhnd"):
+                 stream=None, layout: str = "bhnd", positions=None, axes=None):
     """Norm of each query and key head and rotation by its token's position, in one pass.
 
     q is [B, H, N, d] and k [B, Hkv, N, d] float16 or bfloat16 (``layout="bnhd"``:
@@ -176,7 +201,14 @@ def qk_norm_rope(q, k, cos=None, sin=None, q_weight=None, k_weight=None, eps: fl
     ``counts`` (int32 [B]; None: N): rows of a padded batch past them are written as
     zeros.  A position outside the table gives NaN rows.  Returns (q_out, k_out),
     contiguous in ``layout``, as ``fwd`` and ``fwd_window`` take them
-    (``qm_qk_norm_rope``)."""
+    (``qm_qk_norm_rope``).
+
+    ``positions`` (int32 [A, B, N], A from 1 to 4; instead of ``starts``): positions on
+    several axes, such as time, height and width of a picture's parts.  ``axes``, a
+    sequence of rotary / 2 whole numbers below A (None where A is 1), names the axis of
+    each pair: pair j of token t of sequence b turns by row ``positions[axes[j], b, t]`` of
+    the table's column j.  Places past ``counts``, and axes that no pair has, are not looked
+    at (``qm_qk_norm_rope_axes``)."""
     index, dtype, code = _queries(q)
     lay = _layout_code(layout)
     (B, N, H, d), qs = _rows("q", q, dtype, index, lay)
@@ -187,6 +219,14 @@ def qk_norm_rope(q, k, cos=None, sin=None, q_weight=None, k_weight=None, eps: fl
     torch = _torch()
     qw, kw = _vectors(("q_weight", "k_weight"), q_weight, k_weight, (d,), index, dtype)
     first, held = _vectors(("starts", "counts"), starts, counts, (B,), index, torch.int32)
+    if positions is not None:
+        if starts is not None:
+            raise ValueError("starts must be None where positions are given")
+        entry, at = load_library().qm_qk_norm_rope_axes, _positions(positions, axes, rotary, B, N, index)
+    else:
+        if axes is not None:
+            raise ValueError("axes are given with positions")
+        entry, at = load_library().qm_qk_norm_rope, (first,)
     with _pool_of(stream, q_out is None or k_out is None):
         if q_out is None:
             q_out = _new(torch, q)
@@ -196,8 +236,8 @@ def qk_norm_rope(q, k, cos=None, sin=None, q_weight=None, k_weight=None, eps: fl
             k_out = _new(torch, k)
         else:
             _vector("k_out", k_out, k.shape, index, dtype)
-    _enqueue(load_library().qm_qk_norm_rope, _device(index), stream,
-             (q.data_ptr(), k.data_ptr(), q_out.data_ptr(), k_out.data_ptr(), qw, kw, c, s, first,
+    _enqueue(entry, _device(index), stream,
+             (q.data_ptr(), k.data_ptr(), q_out.data_ptr(), k_out.data_ptr(), qw, kw, c, s, *at,
               held, B, H, Hkv, N, d, rotary, table_rows, float(eps), 1 if interleaved else 0, qs, ks),
              (code, lay))
     return q_out, k_out
@@ -207,7 +247,7 @@ def qk_norm_rope_append(q, k, v, k_cache, v_cache, page_table, starts=None, cos=
                         q_weight=None, k_weight=None, eps: float = 1e-6, counts=None,
                         interleaved: bool = False, k_scale: float = 1.0, v_scale: float = 1.0,
                         q_out=None, k_out=None, stream=None, layout: str = "bhnd",
-                        cache_layout: str = "bhnd"):
+                        cache_layout: str = "bhnd", positions=None, axes=None):
     """:func:`qk_norm_rope`, with the keys and the values v written to a paged cache:
     token t of sequence b at position ``starts[b]`` + t, rows past ``counts`` not at all.
 
@@ -218,7 +258,11 @@ def qk_norm_rope_append(q, k, v, k_cache, v_cache, page_table, starts=None, cos=
     belongs to one sequence and stands once in its row.  v has k's shape and any
     strides as q and k; ``k_out``, where given, receives the keys as ``qk_norm_rope``
     returns them.  Without cos, sin and weights the keys are stored as they are.  Returns
-    q_out (``qm_qk_norm_rope_append``)."""
+    q_out (``qm_qk_norm_rope_append``).
+
+    With ``positions`` and ``axes``, as in :func:`qk_norm_rope`, the rotation takes those,
+    and ``starts`` says only where in the cache a sequence's tokens go
+    (``qm_qk_norm_rope_append_axes``)."""
     index, dtype, code = _queries(q)
     lay = _layout_code(layout)
     (B, N, H, d), qs = _rows("q", q, dtype, index, lay)
@@ -234,6 +278,13 @@ def qk_norm_rope_append(q, k, v, k_cache, v_cache, page_table, starts=None, cos=
     torch = _torch()
     qw, kw = _vectors(("q_weight", "k_weight"), q_weight, k_weight, (d,), index, dtype)
     first, held = _vectors(("starts", "counts"), starts, counts, (B,), index, torch.int32)
+    if positions is not None:
+        entry = load_library().qm_qk_norm_rope_append_axes
+        at = (*_positions(positions, axes, rotary, B, N, index), first)
+    else:
+        if axes is not None:
+            raise ValueError("axes are given with positions")
+        entry, at = load_library().qm_qk_norm_rope_append, (first,)
     if q_out is None:
         with _pool_of(stream, True):
             q_out = _new(torch, q)
@@ -241,13 +292,136 @@ def qk_norm_rope_append(q, k, v, k_cache, v_cache, page_table, starts=None, cos=
         _vector("q_out", q_out, q.shape, index, dtype)
     if k_out is not None:
         k_out = _vector("k_out", k_out, k.shape, index, dtype)
-    _enqueue(load_library().qm_qk_norm_rope_append, _device(index), stream,
+    _enqueue(entry, _device(index), stream,
              (q.data_ptr(), k.data_ptr(), v.data_ptr(), q_out.data_ptr(), k_out, k_cache.data_ptr(),
-              v_cache.data_ptr(), table, qw, kw, c, s, first, held, B, H, Hkv, N, d, rotary,
+              v_cache.data_ptr(), table, qw, kw, c, s, *at, held, B, H, Hkv, N, d, rotary,
               table_rows, float(eps), 1 if interleaved else 0, pages, page_size, table_columns,
               float(k_scale), float(v_scale), qs, ks, vs),
              (code, lay, kind, cache_lay))
     return q_out
+
+
+def _lines(name, t, size, dtype, index):
+    """The elements from row to row of a [..., D] tensor of `size` whose rows lie at equal
+    distances, each contiguous."""
+    if t.shape != size:
+        raise ValueError(f"{name} must have shape {list(size)}, not {list(t.shape)}")
+    if t.dtype is not dtype:
+        raise TypeError(f"{name} must be {dtype}, not {t.dtype}")
+    if t.get_device() != index:
+        raise _elsewhere(name, t, index)
+    if t.is_contiguous():
+        return size[-1]
+    stride, step, next_ = t.stride(), None, 0
+    if size[-1] != 1 and stride[-1] != 1:
+        raise ValueError(f"{name}'s columns must be contiguous")
+    for n, s in zip(reversed(size[:-1]), reversed(stride[:-1])):
+        if n == 1:
+            continue
+        if step is None:
+            step = s
+        elif s != next_:
+            raise ValueError(f"{name}'s rows must lie at equal distances")
+        next_ = s * n
+    return size[-1] if step is None else step
+
+
+def _normed(x, weight, residual, sum_out):
+    """The checks that both norms share: device index, type, its code, rows, width, the
+    strides of x, residual and sum_out, and the weight's address."""
+    if not x.is_cuda:
+        raise ValueError("x must be on a ROCm device")
+    size = x.shape
+    if not size or not x.numel():
+        raise ValueError("x must have shape [..., width], with a row at least")
+    index, dtype, code = x.get_device(), x.dtype, _dtype_code(x, "x")
+    width = size[-1]
+    lines = _lines("x", x, size, dtype, index)
+    if weight is not None:
+        weight = _vector("weight", weight, (width,), index, dtype)
+    further = after = width
+    if residual is not None:
+        further = _lines("residual", residual, size, dtype, index)
+        if sum_out is not None:
+            after = _lines("sum_out", sum_out, size, dtype, index)
+    elif sum_out is not None:
+        raise ValueError("sum_out is given with a residual")
+    rows = _int32(x.numel() // width, "x's number of rows")
+    return index, dtype, code, rows, width, lines, further, after, weight
+
+
+def rms_norm(x, weight=None, residual=None, eps: float = 1e-6, out=None, sum_out=None, stream=None):
+    """Norm of whole rows, of x or of its sum with a residual, in one pass.
+
+    x and ``residual`` (None: none) are [..., width] float16 or bfloat16, width a multiple of
+    8 up to 32768, their rows contiguous and at equal distances of a multiple of 8 elements
+    (views into a wider projection's output, say, or one row expanded).  With s = x + residual,
+    y = s * ``weight`` / sqrt(mean(s^2) + eps) (``weight`` [width], or None), in float32,
+    rounded once.
+
+    Returns (y, sum): y contiguous, and s rounded to x's type (None without a residual).
+    ``sum_out`` may be ``residual`` (or x) itself, whose place the sum then takes.
+    (``qm_rms_norm``)"""
+    index, dtype, code, rows, width, lines, further, after, w = _normed(x, weight, residual, sum_out)
+    torch = _torch()
+    make_sum = residual is not None and sum_out is None
+    with _pool_of(stream, out is None or make_sum):
+        if out is None:
+            out = _new(torch, x)
+        else:
+            _vector("out", out, x.shape, index, dtype)
+        if make_sum:
+            sum_out = _new(torch, x)
+    _enqueue(load_library().qm_rms_norm, _device(index), stream,
+             (x.data_ptr(), None if residual is None else residual.data_ptr(), w, out.data_ptr(),
+              None if sum_out is None else sum_out.data_ptr(), rows, width, lines, further, after,
+              float(eps)), (code,))
+    return out, sum_out
+
+
+def rms_norm_fp8(x, weight=None, residual=None, eps: float = 1e-6, scale: float | None = None,
+                 group: int | None = None, out=None, scales=None, sum_out=None, stream=None):
+    """:func:`rms_norm` with a result of E4M3 codes, y = scale * code.
+
+    ``scale``: one factor for all, as ``fwd_fp8`` takes (y beyond 448 of it as 448).  None:
+    a factor for each row, or for each ``group`` (32, 64, 128 or 256, dividing width) of a
+    row's columns, max |y| / 448 over them, at least 2^-126.
+
+    Returns (codes, scales, sum): ``float8_e4m3fn`` codes shaped like x (``out`` may be
+    uint8), float32 scales [..., 1] or [..., width / group] (None with ``scale``), and the sum
+    as there.  (``qm_rms_norm_fp8``)"""
+    index, dtype, code, rows, width, lines, further, after, w = _normed(x, weight, residual, sum_out)
+    torch = _torch()
+    make_sum = residual is not None and sum_out is None
+    size = x.shape
+    if scale is not None:
+        if group is not None or scales is not None:
+            raise ValueError("scale is one factor for all: group and scales must be None")
+        group = 0
+    else:
+        group = 0 if group is None else _int32(group, "group")
+        if group not in (0, 32, 64, 128, 256) or (group and width % group):
+            raise ValueError("group must be 32, 64, 128 or 256 and divide x's width")
+    with _pool_of(stream, out is None or make_sum or (scale is None and scales is None)):
+        if out is None:
+            out = torch.empty(size, dtype=torch.float8_e4m3fn, device=_device(index))
+        else:
+            _vector("out", out, size, index,
+                    out.dtype if out.dtype is torch.uint8 else torch.float8_e4m3fn)
+        if scale is None:
+            shape = (*size[:-1], width // group if group else 1)
+            if scales is None:
+                scales = torch.empty(shape, dtype=torch.float32, device=_device(index))
+            else:
+                _vector("scales", scales, shape, index, torch.float32)
+        if make_sum:
+            sum_out = _new(torch, x)
+    _enqueue(load_library().qm_rms_norm_fp8, _device(index), stream,
+             (x.data_ptr(), None if residual is None else residual.data_ptr(), w, out.data_ptr(),
+              None if scales is None else scales.data_ptr(),
+              None if sum_out is None else sum_out.data_ptr(), rows, width, lines, further, after,
+              float(eps), 1.0 if scale is None else float(scale), group), (code,))
+    return out, scales, sum_out
 
 
 @functools.lru_cache(maxsize=1024)
