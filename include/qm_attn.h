@@ -524,6 +524,45 @@ int qm_attn_decode(const void* q, const void* k_cache, const void* v_cache, void
 int qm_attn_decode_workspace(int B, int H, int Hkv, int d, int page_size, int table_cols,
                              int max_length, int window, int sinks, size_t* bytes);
 
+/*
+ * qm_attn_decode_shared - qm_attn_decode (without a window) for sequences whose first
+ * prefix_length tokens are the same: the result is that of qm_attn_decode on a cache in which
+ * token t of every sequence is, for t < prefix_length, row t % page_size of page
+ * prefix_table[t / page_size], and from there on as page_table says.  Keys and values of
+ * the prefix are read for many queries at once, not for each sequence.
+ *
+ *   prefix_table [in]  device, [prefix_cols] int32, 4-byte aligned: the prefix's pages in order,
+ *                      prefix_cols * page_size tokens or fewer.  Entries past the prefix's last
+ *                      token are not looked at, nor those of page_table before it.
+ *   prefix_length      0: qm_attn_decode (prefix_table may be NULL).  It need not be a
+ *                      multiple of page_size: a sequence's own tokens then begin inside the
+ *                      page that page_table names for them.
+ *   lengths      [in]  tokens of each sequence, the prefix's among them, as in qm_attn_decode;
+ *                      prefix_length: the prefix alone is visible.  0: o is 0 and lse -infinity.
+ *                      Any other below prefix_length, one above max_length or beyond the page
+ *                      table, or a page out of range among the sequence's: that sequence's
+ *                      o and lse are NaN (with a page of the prefix every sequence's of a
+ *                      length above 0).
+ *   max_length   prefix_length or more (QM_ERR_PAGE).
+ *   workspace    of qm_attn_decode_shared_workspace bytes.
+ *   All other arguments, the arithmetic and the status codes are those of qm_attn_decode.
+ *   Two kernels are enqueued.
+ */
+int qm_attn_decode_shared(const void* q, const void* k_cache, const void* v_cache, void* o,
+                          float* lse, const int* page_table, const int* lengths,
+                          const int* prefix_table, int B, int H, int Hkv, int d, int num_pages,
+                          int page_size, int table_cols, int prefix_cols, int prefix_length,
+                          int max_length, float scale, float k_scale, float v_scale,
+                          void* workspace, size_t workspace_bytes, hipStream_t stream, int dtype,
+                          int cache_dtype, int cache_layout);
+
+/*
+ * qm_attn_decode_shared_workspace - the workspace of a qm_attn_decode_shared call with these
+ * arguments on the current device, in bytes, into *bytes.  Returns a status.
+ */
+int qm_attn_decode_shared_workspace(int B, int H, int Hkv, int d, int page_size, int table_cols,
+                                    int prefix_length, int max_length, size_t* bytes);
+
 /* qm_attn_strerror - a static, human-readable string for a status code. */
 const char* qm_attn_strerror(int status);
 

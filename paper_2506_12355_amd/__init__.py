@@ -56,6 +56,8 @@ from .binding import (  # noqa: F401
 from .serving import (  # noqa: F401
     QM_E4M3,
     decode,
+    decode_shared,
+    decode_shared_workspace,
     decode_workspace,
     qk_norm_rope,
     qk_norm_rope_append,

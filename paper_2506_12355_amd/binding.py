@@ -125,6 +125,11 @@ def _declare(lib: ctypes.CDLL) -> ctypes.CDLL:
     lib.qm_attn_decode.restype = ctypes.c_int
     lib.qm_attn_decode_workspace.argtypes = [I] * 9 + [P]
     lib.qm_attn_decode_workspace.restype = ctypes.c_int
+    lib.qm_attn_decode_shared.argtypes = (
+        [P] * 8 + [I] * 10 + [F] * 3 + [P, ctypes.c_size_t, P] + [I] * 3)
+    lib.qm_attn_decode_shared.restype = ctypes.c_int
+    lib.qm_attn_decode_shared_workspace.argtypes = [I] * 8 + [P]
+    lib.qm_attn_decode_shared_workspace.restype = ctypes.c_int
     lib.qm_attn_set_tile_rows.argtypes = [ctypes.c_int]
     lib.qm_attn_set_tile_rows.restype = ctypes.c_int
     lib.qm_attn_strerror.argtypes = [ctypes.c_int]

@@ -31,7 +31,7 @@ SOURCES = ["qm_attn.cpp", "attn_fwd_gfx950.hip", "attn_fwd_split_gfx950.hip",
 # The operators around the attention forward, in a folder of their own.  Their kernels
 # keep NaNs apart (an unusable position or page gives NaN rows, and E4M3 codes of NaN).
 SERVING_SOURCES = ["serving/qm_serving.cpp", "serving/norm_rope.hip", "serving/rms_norm.hip",
-                   "serving/decode.hip"]
+                   "serving/decode.hip", "serving/shared.hip"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950",

@@ -12,6 +12,7 @@
 #include "checks.h"
 #include "decode_rules.h"
 #include "serving_launch.h"
+#include "shared_rules.h"
 
 namespace {
 
@@ -297,11 +298,105 @@ int plan(int B, int H, int Hkv, int d, int page_size, int table_cols, int max_le
   return QM_OK;
 }
 
+// The same for a call behind a shared prefix of at least one token.
+int plan_shared(int B, int H, int Hkv, int d, int page_size, int table_cols, int prefix,
+                int max_length, qm::SharedPlan* p, int* limit) {
+  qm::DecodePlan unused;
+  const int st = plan(B, H, Hkv, d, page_size, table_cols, max_length, 0, 0, &unused, limit);
+  if (st != QM_OK) return st;
+  // the longest a sequence can be; its own pages may end before the prefix does
+  if (prefix < 1 || prefix > kMostTokens || prefix > max_length) return QM_ERR_PAGE;
+  if (*limit < prefix) *limit = prefix;
+  *p = qm::plan_shared(B, H, Hkv, *limit, prefix, device_cus());
+  return QM_OK;
+}
+
 // Two partial results of 16 heads for each workgroup of a call in shares, and two
 // numbers for each row.
 size_t workspace_of(const qm::DecodePlan& p, int B, int H, int Hkv, int d) {
   const size_t rows = (size_t)B * Hkv * ((H / Hkv + 15) / 16);
   return p.grid ? (size_t)2 * p.grid * 16 * (d + 2) * sizeof(float) + rows * 2 * sizeof(int32_t) : 0;
+}
+
+// A partial result of 16 queries for each part of each of the prefix's tiles, then those
+// of the sequences' own tokens and two numbers for each of their rows.
+size_t workspace_of(const qm::SharedPlan& p, int B, int H, int Hkv, int d) {
+  const size_t slots = (size_t)Hkv * p.tiles * p.rt * p.splits + qm::own_slots(p, B, H, Hkv);
+  const size_t rows = p.own_grid ? (size_t)B * Hkv * ((H / Hkv + 15) / 16) : 0;
+  return slots * 16 * (d + 2) * sizeof(float) + rows * 2 * sizeof(int32_t);
+}
+
+// Both entry points; shared: the one with a prefix of `prefix` tokens in prefix_table.
+int decode(const void* q, const void* k_cache, const void* v_cache, void* o, float* lse,
+           const int* page_table, const int* lengths, const int* prefix_table, int B, int H, int Hkv,
+           int d, int num_pages, int page_size, int table_cols, int prefix_cols, int prefix,
+           int max_length, float scale, float k_scale, float v_scale, int window, int sinks,
+           void* workspace, size_t workspace_bytes, hipStream_t stream, int dtype, int cache_dtype,
+           int cache_layout) {
+  if (!q || !k_cache || !v_cache || !o || !lse || !page_table || !lengths) return QM_ERR_NULL;
+  if (prefix && !prefix_table) return QM_ERR_NULL;
+  if (dtype != QM_F16 && dtype != QM_BF16) return QM_ERR_DTYPE;
+  if (B < 1 || H < 1 || Hkv < 1 || Hkv > H || H % Hkv != 0) return QM_ERR_SHAPE;
+  if (d != 64 && d != 128) return QM_ERR_HEADDIM;
+  qm::DecodeArgs a = {};
+  uint64_t cache_bytes = 0;
+  int st = check_cache(&a.cache, &cache_bytes, Hkv, d, num_pages, page_size, table_cols, dtype,
+                       cache_dtype, cache_layout);
+  if (st != QM_OK) return st;
+  if (max_length < 1 || prefix < 0) return QM_ERR_PAGE;
+  if (prefix && (prefix_cols < 1 || (int64_t)prefix_cols * page_size > kMostTokens ||
+                 (int64_t)prefix_cols * page_size < prefix))
+    return QM_ERR_PAGE;
+  if (window < 0 || sinks < 0) return QM_ERR_WINDOW;
+  const double c = (double)scale * (double)k_scale * 1.4426950408889634074;
+  if (!finite_bits(scale) || !finite_bits(k_scale) || !finite_bits(v_scale) ||
+      !(fabs(c) < (double)FLT_MAX))
+    return QM_ERR_SCALE;
+  const uint64_t rows = times((uint64_t)B, (uint64_t)H);
+  if (rows > INT_MAX / 256) return QM_ERR_SHAPE;
+  const Range in[] = {{q, rows * d * 2}, {k_cache, cache_bytes}, {v_cache, cache_bytes},
+                      {page_table, (uint64_t)B * (uint64_t)table_cols * 4}, {lengths, (uint64_t)B * 4},
+                      {prefix ? prefix_table : nullptr, prefix ? (uint64_t)prefix_cols * 4 : 0}};
+  const Range ro = {o, rows * d * 2}, rl = {lse, rows * 4};
+  if (any_overlap(ro, in) || any_overlap(rl, in) || overlaps(o, ro.bytes, lse, rl.bytes))
+    return QM_ERR_ALIAS;
+  if (!aligned16(q) || !aligned16(k_cache) || !aligned16(v_cache) || !aligned16(o) ||
+      !aligned16(lse) || !aligned4(page_table) || !aligned4(lengths) || (prefix && !aligned4(prefix_table)))
+    return QM_ERR_UNSUPPORTED;
+  qm::DecodePlan p;
+  qm::SharedPlan s;
+  st = prefix ? plan_shared(B, H, Hkv, d, page_size, table_cols, prefix, max_length, &s, &a.limit)
+              : plan(B, H, Hkv, d, page_size, table_cols, max_length, window, sinks, &p, &a.limit);
+  if (st != QM_OK) return st;
+  const size_t need = prefix ? workspace_of(s, B, H, Hkv, d) : workspace_of(p, B, H, Hkv, d);
+  if (need) {
+    if (!workspace || workspace_bytes < need) return QM_ERR_WORKSPACE;
+    const Range rw = {workspace, need};
+    if (any_overlap(rw, in) || overlaps(workspace, need, o, ro.bytes) ||
+        overlaps(workspace, need, lse, rl.bytes))
+      return QM_ERR_ALIAS;
+    if (!aligned16(workspace)) return QM_ERR_UNSUPPORTED;
+  }
+  a.q = static_cast<const uint16_t*>(q);
+  a.o = static_cast<uint16_t*>(o);
+  a.lse = lse;
+  a.lengths = lengths;
+  a.cache.k = const_cast<void*>(k_cache);
+  a.cache.v = const_cast<void*>(v_cache);
+  a.cache.table = page_table;
+  a.B = B;
+  a.H = H;
+  a.Hkv = Hkv;
+  a.d = d;
+  a.dtype = dtype;
+  a.window = window;
+  a.sinks = sinks;
+  a.c = (float)c;
+  a.v_scale = v_scale;
+  a.workspace = static_cast<float*>(workspace);
+  const hipError_t e = prefix ? qm::launch_shared({a, prefix_table, prefix}, s, stream)
+                              : qm::launch_decode(a, p, stream);
+  return e == hipSuccess ? QM_OK : QM_ERR_LAUNCH;
 }
 
 }  // namespace
@@ -395,59 +490,33 @@ extern "C" int qm_attn_decode(const void* q, const void* k_cache, const void* v_
                               int max_length, float scale, float k_scale, float v_scale, int window,
                               int sinks, void* workspace, size_t workspace_bytes, hipStream_t stream,
                               int dtype, int cache_dtype, int cache_layout) {
-  if (!q || !k_cache || !v_cache || !o || !lse || !page_table || !lengths) return QM_ERR_NULL;
-  if (dtype != QM_F16 && dtype != QM_BF16) return QM_ERR_DTYPE;
-  if (B < 1 || H < 1 || Hkv < 1 || Hkv > H || H % Hkv != 0) return QM_ERR_SHAPE;
-  if (d != 64 && d != 128) return QM_ERR_HEADDIM;
-  qm::DecodeArgs a = {};
-  uint64_t cache_bytes = 0;
-  int st = check_cache(&a.cache, &cache_bytes, Hkv, d, num_pages, page_size, table_cols, dtype,
-                       cache_dtype, cache_layout);
-  if (st != QM_OK) return st;
-  if (max_length < 1) return QM_ERR_PAGE;
-  if (window < 0 || sinks < 0) return QM_ERR_WINDOW;
-  const double c = (double)scale * (double)k_scale * 1.4426950408889634074;
-  if (!finite_bits(scale) || !finite_bits(k_scale) || !finite_bits(v_scale) ||
-      !(fabs(c) < (double)FLT_MAX))
-    return QM_ERR_SCALE;
-  const uint64_t rows = times((uint64_t)B, (uint64_t)H);
-  if (rows > INT_MAX / 256) return QM_ERR_SHAPE;
-  const Range in[] = {{q, rows * d * 2}, {k_cache, cache_bytes}, {v_cache, cache_bytes},
-                      {page_table, (uint64_t)B * (uint64_t)table_cols * 4}, {lengths, (uint64_t)B * 4}};
-  const Range ro = {o, rows * d * 2}, rl = {lse, rows * 4};
-  if (any_overlap(ro, in) || any_overlap(rl, in) || overlaps(o, ro.bytes, lse, rl.bytes))
-    return QM_ERR_ALIAS;
-  if (!aligned16(q) || !aligned16(k_cache) || !aligned16(v_cache) || !aligned16(o) ||
-      !aligned16(lse) || !aligned4(page_table) || !aligned4(lengths))
-    return QM_ERR_UNSUPPORTED;
-  qm::DecodePlan p;
-  st = plan(B, H, Hkv, d, page_size, table_cols, max_length, window, sinks, &p, &a.limit);
-  if (st != QM_OK) return st;
-  const size_t need = workspace_of(p, B, H, Hkv, d);
-  if (need) {
-    if (!workspace || workspace_bytes < need) return QM_ERR_WORKSPACE;
-    const Range rw = {workspace, need};
-    if (any_overlap(rw, in) || overlaps(workspace, need, o, ro.bytes) ||
-        overlaps(workspace, need, lse, rl.bytes))
-      return QM_ERR_ALIAS;
-    if (!aligned16(workspace)) return QM_ERR_UNSUPPORTED;
-  }
-  a.q = static_cast<const uint16_t*>(q);
-  a.o = static_cast<uint16_t*>(o);
-  a.lse = lse;
-  a.lengths = lengths;
-  a.cache.k = const_cast<void*>(k_cache);
-  a.cache.v = const_cast<void*>(v_cache);
-  a.cache.table = page_table;
-  a.B = B;
-  a.H = H;
-  a.Hkv = Hkv;
-  a.d = d;
-  a.dtype = dtype;
-  a.window = window;
-  a.sinks = sinks;
-  a.c = (float)c;
-  a.v_scale = v_scale;
-  a.workspace = static_cast<float*>(workspace);
-  return qm::launch_decode(a, p, stream) == hipSuccess ? QM_OK : QM_ERR_LAUNCH;
+  return decode(q, k_cache, v_cache, o, lse, page_table, lengths, nullptr, B, H, Hkv, d, num_pages,
+                page_size, table_cols, 0, 0, max_length, scale, k_scale, v_scale, window, sinks,
+                workspace, workspace_bytes, stream, dtype, cache_dtype, cache_layout);
+}
+
+extern "C" int qm_attn_decode_shared_workspace(int B, int H, int Hkv, int d, int page_size,
+                                               int table_cols, int prefix_length, int max_length,
+                                               size_t* bytes) {
+  if (!bytes) return QM_ERR_NULL;
+  if (prefix_length == 0)
+    return qm_attn_decode_workspace(B, H, Hkv, d, page_size, table_cols, max_length, 0, 0, bytes);
+  qm::SharedPlan p;
+  int limit;
+  const int st = plan_shared(B, H, Hkv, d, page_size, table_cols, prefix_length, max_length, &p, &limit);
+  if (st == QM_OK) *bytes = workspace_of(p, B, H, Hkv, d);
+  return st;
+}
+
+extern "C" int qm_attn_decode_shared(const void* q, const void* k_cache, const void* v_cache, void* o,
+                                     float* lse, const int* page_table, const int* lengths,
+                                     const int* prefix_table, int B, int H, int Hkv, int d,
+                                     int num_pages, int page_size, int table_cols, int prefix_cols,
+                                     int prefix_length, int max_length, float scale, float k_scale,
+                                     float v_scale, void* workspace, size_t workspace_bytes,
+                                     hipStream_t stream, int dtype, int cache_dtype,
+                                     int cache_layout) {
+  return decode(q, k_cache, v_cache, o, lse, page_table, lengths, prefix_table, B, H, Hkv, d, num_pages,
+                page_size, table_cols, prefix_cols, prefix_length, max_length, scale, k_scale, v_scale,
+                0, 0, workspace, workspace_bytes, stream, dtype, cache_dtype, cache_layout);
 }

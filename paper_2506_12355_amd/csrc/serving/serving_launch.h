@@ -70,4 +70,19 @@ struct DecodePlan {
 
 hipError_t launch_decode(const DecodeArgs& a, const DecodePlan& plan, hipStream_t stream);
 
+struct SharedArgs {
+  DecodeArgs decode;            // window and sinks 0
+  const int32_t* prefix_table;  // pages of the first `prefix` tokens, for all sequences
+  int prefix;
+};
+
+// How a call behind a shared prefix is divided: the prefix into `splits` parts for each
+// tile of 16 rt queries of a key/value head, and equal shares of the sequences' own blocks for
+// own_grid workgroups (0: there can be none), in one launch of prefix_grid + own_grid.
+struct SharedPlan {
+  int rt, tiles, splits, prefix_grid, own_grid;
+};
+
+hipError_t launch_shared(const SharedArgs& a, const SharedPlan& plan, hipStream_t stream);
+
 }  // namespace qm

@@ -425,12 +425,13 @@ def rms_norm_fp8(x, weight=None, residual=None, eps: float = 1e-6, scale: float 
 
 
 @functools.lru_cache(maxsize=1024)
-def _workspace_bytes(index, *sizes) -> int:
-    """Workspace of a decode call of these sizes on device `index` (sizes alone decide)."""
+def _workspace_bytes(entry, index, *sizes) -> int:
+    """Workspace of a decode call of these sizes on device `index` (sizes alone decide), of
+    which the library's `entry` tells."""
     import torch
     need = ctypes.c_size_t()
     with torch.cuda.device(index):
-        status = load_library().qm_attn_decode_workspace(*sizes, ctypes.byref(need))
+        status = getattr(load_library(), entry)(*sizes, ctypes.byref(need))
     if status != QM_OK:
         raise QmAttnError(status, strerror(status))
     return need.value
@@ -445,7 +446,7 @@ def decode_workspace(q, k_cache, page_table, max_length: int | None = None,
     B, H, d = q.shape
     _, page_size, heads, columns, _, _, _ = _cache(k_cache, k_cache, page_table, B, d, dtype, code,
                                                 index, cache_layout)
-    return _workspace_bytes(index, B, H, heads, d, page_size, columns,
+    return _workspace_bytes("qm_attn_decode_workspace", index, B, H, heads, d, page_size, columns,
                             _MOST if max_length is None else _int32(max_length, "max_length"),
                             0 if window is None else _window(window), _int32(sinks, "sinks"))
 
@@ -476,6 +477,15 @@ def decode(q, k_cache, v_cache, page_table, lengths, scale: float | None = None,
     faster.  ``workspace``: a uint8 tensor of :func:`decode_workspace` bytes (None: one is
     allocated on the call's stream); two calls that may run at once need one each.
     ``scale`` defaults to 1/sqrt(d) rounded to float32.  (``qm_attn_decode``)"""
+    return _decode(q, k_cache, v_cache, page_table, lengths, scale, k_scale, v_scale, max_length, out, lse,
+                   workspace, stream, cache_layout,
+                   window=(0 if window is None else _window(window), _int32(sinks, "sinks")))
+
+
+def _decode(q, k_cache, v_cache, page_table, lengths, scale, k_scale, v_scale, max_length, out, lse,
+            workspace, stream, cache_layout, window=None, prefix=None):
+    """Both decoding calls: with a window and first keys, or with a prefix's page table and
+    length."""
     index, dtype, code = _queries(q)
     if q.dim() != 3 or not q.is_contiguous():
         raise ValueError("q must be a contiguous [B, H, d] tensor")
@@ -487,8 +497,18 @@ def decode(q, k_cache, v_cache, page_table, lengths, scale: float | None = None,
         raise ValueError("lengths must be given")
     lens = _vector("lengths", lengths, (B,), index, torch.int32)
     scale = 1.0 / d ** 0.5 if scale is None else float(scale)   # rounded to float32 by the call
-    window = 0 if window is None else _window(window)
-    sinks = _int32(sinks, "sinks")
+    if prefix is not None:
+        prefix_table, prefix_length = prefix
+        prefix_length = _int32(prefix_length, "prefix_length")
+        if prefix_length < 0:
+            raise ValueError("prefix_length must be 0 or more")
+        if prefix_table is None:
+            if prefix_length:
+                raise ValueError("prefix_table must be given with a prefix")
+            pages_of_prefix, prefix_columns = None, 0
+        else:
+            prefix_columns = prefix_table.numel()
+            pages_of_prefix = _vector("prefix_table", prefix_table, (prefix_columns,), index, torch.int32)
     most = _MOST if max_length is None else _int32(max_length, "max_length")
     with _pool_of(stream, out is None or lse is None or workspace is None):
         if out is None:
@@ -499,7 +519,12 @@ def decode(q, k_cache, v_cache, page_table, lengths, scale: float | None = None,
             lse = torch.empty(B, H, dtype=torch.float32, device=_device(index))
         else:
             _vector("lse", lse, (B, H), index, torch.float32)
-        need = _workspace_bytes(index, B, H, Hkv, d, page_size, columns, most, window, sinks)
+        if prefix is None:
+            need = _workspace_bytes("qm_attn_decode_workspace", index, B, H, Hkv, d, page_size, columns,
+                                    most, *window)
+        else:
+            need = _workspace_bytes("qm_attn_decode_shared_workspace", index, B, H, Hkv, d, page_size,
+                                    columns, prefix_length, most)
         if workspace is not None:
             if workspace.dtype is not torch.uint8 or workspace.dim() != 1 or not workspace.is_contiguous():
                 raise ValueError("workspace must be a contiguous 1-D uint8 tensor")
@@ -511,9 +536,53 @@ def decode(q, k_cache, v_cache, page_table, lengths, scale: float | None = None,
             ws, given = workspace.data_ptr(), need
         else:
             ws, given = None, 0
-    _enqueue(load_library().qm_attn_decode, _device(index), stream,
-             (q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), out.data_ptr(), lse.data_ptr(),
-              table, lens, B, H, Hkv, d, pages, page_size, columns, most, scale,
-              float(k_scale), float(v_scale), window, sinks, ws, given),
-             (code, kind, cache_lay))
+    tensors = (q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), out.data_ptr(), lse.data_ptr(),
+               table, lens)
+    if prefix is None:
+        _enqueue(load_library().qm_attn_decode, _device(index), stream,
+                 (*tensors, B, H, Hkv, d, pages, page_size, columns, most, scale, float(k_scale),
+                  float(v_scale), *window, ws, given),
+                 (code, kind, cache_lay))
+    else:
+        _enqueue(load_library().qm_attn_decode_shared, _device(index), stream,
+                 (*tensors, pages_of_prefix, B, H, Hkv, d, pages, page_size, columns, prefix_columns,
+                  prefix_length, most, scale, float(k_scale), float(v_scale), ws, given),
+                 (code, kind, cache_lay))
     return out, lse
+
+
+def decode_shared_workspace(q, k_cache, page_table, prefix_length: int, max_length: int | None = None,
+                            cache_layout: str = "bhnd") -> int:
+    """Bytes of workspace that :func:`decode_shared` needs for these arguments."""
+    index, dtype, code = _queries(q)
+    if q.dim() != 3:
+        raise ValueError("q must have shape [B, H, d]")
+    B, H, d = q.shape
+    _, page_size, heads, columns, _, _, _ = _cache(k_cache, k_cache, page_table, B, d, dtype, code,
+                                                index, cache_layout)
+    return _workspace_bytes("qm_attn_decode_shared_workspace", index, B, H, heads, d, page_size, columns,
+                            _int32(prefix_length, "prefix_length"),
+                            _MOST if max_length is None else _int32(max_length, "max_length"))
+
+
+def decode_shared(q, k_cache, v_cache, page_table, lengths, prefix_table, prefix_length: int,
+                  scale: float | None = None, k_scale: float = 1.0, v_scale: float = 1.0,
+                  max_length: int | None = None, out=None, lse=None, workspace=None, stream=None,
+                  cache_layout: str = "bhnd"):
+    """:func:`decode` for sequences that share their first ``prefix_length`` tokens, whose
+    pages ``prefix_table`` (int32 [columns]) names for all of them: what is read of the
+    prefix is read for many queries at once.
+
+    ``lengths`` counts all of a sequence's tokens, the prefix's among them.  Token t of a
+    sequence from ``prefix_length`` on is in page ``page_table[b, t // page_size]``, as for
+    ``decode``; entries for earlier tokens are not looked at.  ``prefix_length`` need not be
+    a multiple of the page size, and 0 is ``decode`` (``prefix_table`` may then be None).
+
+    Returns (o [B, H, d], lse float32 [B, H]).  Length 0 (a free slot) gives o = 0 and lse
+    = -inf; any other length below ``prefix_length`` gives NaN, as do the lengths and page
+    numbers out of range that do for ``decode`` (a page of the prefix for every sequence).
+    ``workspace``: as for ``decode``, of :func:`decode_shared_workspace` bytes.  For
+    layers with a window call ``decode``, with the prefix's pages in each sequence's row.
+    (``qm_attn_decode_shared``)"""
+    return _decode(q, k_cache, v_cache, page_table, lengths, scale, k_scale, v_scale, max_length, out, lse,
+                   workspace, stream, cache_layout, prefix=(prefix_table, prefix_length))

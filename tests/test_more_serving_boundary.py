@@ -124,6 +124,52 @@ def test_append_axes_refusals(lib, over, status):
     assert _call(lib.qm_qk_norm_rope_append_axes, APPEND, over) == status
 
 
+def _shared(defaults):
+    args = {}
+    for name, value in defaults.items():
+        if name in ("window", "sinks"):
+            continue
+        if name == "B":
+            args["prefix_table"] = 13 * GIB
+        if name == "max_length":
+            args.update(prefix_cols=5, prefix_length=70)
+        args[name] = value
+    return args
+
+
+SHARED = _shared(tsb.DECODE)
+
+
+@pytest.mark.parametrize("over,status", [
+    (dict(q=None), qa.QM_ERR_NULL), (dict(k_cache=None), qa.QM_ERR_NULL), (dict(v_cache=None), qa.QM_ERR_NULL),
+    (dict(o=None), qa.QM_ERR_NULL), (dict(lse=None), qa.QM_ERR_NULL), (dict(page_table=None), qa.QM_ERR_NULL),
+    (dict(lengths=None), qa.QM_ERR_NULL), (dict(prefix_table=None), qa.QM_ERR_NULL), (dict(dtype=2), qa.QM_ERR_DTYPE),
+    (dict(B=0), qa.QM_ERR_SHAPE), (dict(H=7), qa.QM_ERR_SHAPE), (dict(d=192), qa.QM_ERR_HEADDIM), (dict(page_size=20), qa.QM_ERR_PAGE),
+    (dict(prefix_length=-1), qa.QM_ERR_PAGE), (dict(prefix_length=81), qa.QM_ERR_PAGE), (dict(prefix_cols=0), qa.QM_ERR_PAGE),
+    (dict(prefix_cols=1 << 30), qa.QM_ERR_PAGE), (dict(prefix_cols=-3), qa.QM_ERR_PAGE),
+    (dict(cache_layout=2), qa.QM_ERR_LAYOUT), (dict(scale=INF), qa.QM_ERR_SCALE), (dict(scale=3e38, k_scale=2.0), qa.QM_ERR_SCALE),
+    (dict(o=1 * GIB), qa.QM_ERR_ALIAS), (dict(o=13 * GIB - 16), qa.QM_ERR_ALIAS), (dict(lse=13 * GIB), qa.QM_ERR_ALIAS),
+    (dict(lengths=7 * GIB + 1), qa.QM_ERR_UNSUPPORTED), (dict(prefix_table=13 * GIB + 2), qa.QM_ERR_UNSUPPORTED),
+    # without a prefix its table is not looked at, whatever its address and columns
+    (dict(prefix_length=0, prefix_table=4 * GIB + 1, prefix_cols=-1, lengths=7 * GIB + 1), qa.QM_ERR_UNSUPPORTED),
+    (dict(prefix_length=0, prefix_table=None, prefix_cols=0, lengths=7 * GIB + 1), qa.QM_ERR_UNSUPPORTED),
+], ids=str)
+def test_decode_shared_refusals(lib, over, status):
+    assert _call(lib.qm_attn_decode_shared, SHARED, over) == status
+
+
+def test_shared_workspace_refusals(lib):
+    need = ctypes.c_size_t(77)
+    good = dict(B=2, H=8, Hkv=2, d=128, page_size=16, table_cols=10, prefix_length=70, max_length=100)
+    for over, status in [(dict(B=0), qa.QM_ERR_SHAPE), (dict(Hkv=3), qa.QM_ERR_SHAPE), (dict(d=32), qa.QM_ERR_HEADDIM),
+                         (dict(page_size=15), qa.QM_ERR_PAGE), (dict(table_cols=0), qa.QM_ERR_PAGE), (dict(max_length=0), qa.QM_ERR_PAGE)]:
+        for prefix in (70, 0):
+            args = dict(good, prefix_length=prefix, **over)
+            assert lib.qm_attn_decode_shared_workspace(*args.values(), ctypes.byref(need)) == status
+    assert lib.qm_attn_decode_shared_workspace(*good.values(), None) == qa.QM_ERR_NULL
+    assert need.value == 77
+
+
 def test_status_texts(lib):
     codes = [qa.QM_ERR_NORM, qa.QM_ERR_AXES, qa.QM_ERR_WORKSPACE]
     texts = {qa.strerror(c) for c in codes}
