@@ -78,9 +78,10 @@ struct SharedArgs {
 
 // How a call behind a shared prefix is divided: the prefix into `splits` parts for each
 // tile of 16 rt queries of a key/value head, and equal shares of the sequences' own blocks for
-// own_grid workgroups (0: there can be none), in one launch of prefix_grid + own_grid.
+// own_grid workgroups (0: there can be none), in one launch of prefix_grid + own_grid; then
+// join_threads threads for each head.
 struct SharedPlan {
-  int rt, tiles, splits, prefix_grid, own_grid;
+  int rt, tiles, splits, prefix_grid, own_grid, join_threads;
 };
 
 hipError_t launch_shared(const SharedArgs& a, const SharedPlan& plan, hipStream_t stream);
