@@ -35,6 +35,8 @@ struct Stream {
   int64_t sb, sn, sh;     // input strides, elements
   FastDiv inner, outer;   // of a row index, in the order of the output
   uint32_t rows, units;
+  FastDiv blocks, head_blocks;   // of a unit's index, where a lane has several heads
+  uint32_t batches;
   float inv;              // cached values are multiplied by this
 };
 
@@ -69,7 +71,7 @@ __device__ __forceinline__ float row_sum(float x) {
 }
 
 // The rows of one unit of q (KIND 0), k (1) or v (2).
-template <int DT, int D, bool AXES, int KIND>
+template <int DT, int D, bool AXES, int HEADS, int KIND>
 __device__ __forceinline__ void unit_rows(const Params& p, const Stream& s, uint32_t unit) {
   using T = Type16<DT>;
   constexpr int L = D / 16;      // lanes of a row
@@ -89,10 +91,25 @@ __device__ __forceinline__ void unit_rows(const Params& p, const Stream& s, uint
     w1 = *reinterpret_cast<const u32x4*>(s.weight + c1);
   }
 
-  const uint32_t row = unit * R + lane / L;
-  if (row >= s.rows) return;
-  uint32_t b, h, t;
-  if (p.bnhd) {
+  uint32_t row = unit * R + lane / L, b, h, t;
+  const uint32_t heads = p.bnhd ? s.inner.d : s.outer.d;
+  if (HEADS > 1) {
+    // a lane's rows: of one token, HEADS heads, R apart (a wavefront has R * HEADS of a token) or
+    // neighbours (it has those of R tokens)
+    const uint32_t token = p.bnhd ? s.blocks.div(unit) : 0, block = p.bnhd ? unit - token * s.blocks.d : s.blocks.div(unit);
+    if (p.bnhd) {
+      b = s.outer.div(token);
+      t = token - b * s.outer.d;
+      h = block * (R * HEADS) + lane / L;
+    } else {   // blocks of R tokens the inner index, blocks of HEADS heads the next
+      t = (unit - block * s.blocks.d) * R + lane / L;
+      b = s.head_blocks.div(block);
+      h = (block - b * s.head_blocks.d) * HEADS;
+    }
+    if (b >= s.batches || h >= heads || t >= (uint32_t)p.N) return;
+  } else if (row >= s.rows) {
+    return;
+  } else if (p.bnhd) {
     const uint32_t token = s.inner.div(row);
     h = row - token * s.inner.d;
     b = s.outer.div(token);
@@ -117,130 +134,151 @@ __device__ __forceinline__ void unit_rows(const Params& p, const Stream& s, uint
     fits = inside(row0) && inside(row1) && inside(row2) && inside(row3);
   }
 
-  float x[8], y[8];
-  if (held) {
-    const uint16_t* src = s.x + (int64_t)b * s.sb + (int64_t)t * s.sn + (int64_t)h * s.sh;
-    const u32x4 r0 = *reinterpret_cast<const u32x4*>(src + c0);
-    const u32x4 r1 = *reinterpret_cast<const u32x4*>(src + c1);
+  f32x4 cv[2], sv[2];   // of this lane's pairs
+  auto load_angles = [&]() __attribute__((always_inline)) {
+    int64_t line = at;
+    bool one = true;   // the lane's pairs lie in one row of the table
+    if (AXES) {
+      // the axes of pairs 8 i .. 8 i + 7
+      const uint32_t of = (uint32_t)(p.pair_axis[i >= 4] >> (16 * (i & 3))) & 0xffffu;
+      auto row_of = [&](uint32_t a) __attribute__((always_inline)) {
+        const int low = a & 1 ? row1 : row0, high = a & 1 ? row3 : row2;
+        return a & 2 ? high : low;
+      };
+      line = row_of(of & 3);
+      one = of == (of & 3) * 0x5555u;
+      if (!one) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const f32x2 e0 = T::unpack(r0[j]), e1 = T::unpack(r1[j]);
-      x[2 * j] = e0[0], x[2 * j + 1] = e0[1];
-      y[2 * j] = e1[0], y[2 * j + 1] = e1[1];
-    }
-    if (normed) {
-      float sum = 0.f;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) sum = fmaf(x[j], x[j], fmaf(y[j], y[j], sum));
-      const float r = 1.0f / sqrtf(row_sum<L>(sum) * (1.0f / D) + p.eps);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const f32x2 e0 = T::unpack(w0[j]), e1 = T::unpack(w1[j]);
-        x[2 * j] *= r * e0[0], x[2 * j + 1] *= r * e0[1];
-        y[2 * j] *= r * e1[0], y[2 * j + 1] *= r * e1[1];
+        for (int j = 0; j < 8; ++j) {
+          const int64_t from = (int64_t)row_of(of >> (2 * j) & 3) * half + 8 * i + j;
+          cv[j / 4][j % 4] = p.cos[from];
+          sv[j / 4][j % 4] = p.sin[from];
+        }
       }
     }
-    if (turned && fits) {
-      f32x4 cv[2], sv[2];
-      int64_t line = at;
-      bool one = true;   // the lane's pairs lie in one row of the table
-      if (AXES) {
-        // the axes of pairs 8 i .. 8 i + 7
-        const uint32_t of = (uint32_t)(p.pair_axis[i >= 4] >> (16 * (i & 3))) & 0xffffu;
-        auto row_of = [&](uint32_t a) __attribute__((always_inline)) {
-          const int low = a & 1 ? row1 : row0, high = a & 1 ? row3 : row2;
-          return a & 2 ? high : low;
-        };
-        line = row_of(of & 3);
-        one = of == (of & 3) * 0x5555u;
-        if (!one) {
+    if (one) {
+      const float* ct = p.cos + line * half + 8 * i;
+      const float* st = p.sin + line * half + 8 * i;
 #pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            const int64_t from = (int64_t)row_of(of >> (2 * j) & 3) * half + 8 * i + j;
-            cv[j / 4][j % 4] = p.cos[from];
-            sv[j / 4][j % 4] = p.sin[from];
+      for (int j = 0; j < 2; ++j) {
+        cv[j] = reinterpret_cast<const f32x4*>(ct)[j];
+        sv[j] = reinterpret_cast<const f32x4*>(st)[j];
+      }
+    }
+  };
+  auto one_row = [&](uint32_t row, uint32_t h) __attribute__((always_inline)) {
+    float x[8], y[8];
+    if (held) {
+      const uint16_t* src = s.x + (int64_t)b * s.sb + (int64_t)t * s.sn + (int64_t)h * s.sh;
+      const u32x4 r0 = *reinterpret_cast<const u32x4*>(src + c0);
+      const u32x4 r1 = *reinterpret_cast<const u32x4*>(src + c1);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const f32x2 e0 = T::unpack(r0[j]), e1 = T::unpack(r1[j]);
+        x[2 * j] = e0[0], x[2 * j + 1] = e0[1];
+        y[2 * j] = e1[0], y[2 * j + 1] = e1[1];
+      }
+      if (normed) {
+        float sum = 0.f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) sum = fmaf(x[j], x[j], fmaf(y[j], y[j], sum));
+        const float r = 1.0f / sqrtf(row_sum<L>(sum) * (1.0f / D) + p.eps);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const f32x2 e0 = T::unpack(w0[j]), e1 = T::unpack(w1[j]);
+          x[2 * j] *= r * e0[0], x[2 * j + 1] *= r * e0[1];
+          y[2 * j] *= r * e1[0], y[2 * j + 1] *= r * e1[1];
+        }
+      }
+      if (turned && fits) {
+        if (HEADS == 1) load_angles();
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const float cj = cv[j / 4][j % 4], sj = sv[j / 4][j % 4];
+          if (p.interleaved) {
+            float* z = j < 4 ? x : y;
+            const int e = 2 * (j % 4);
+            const float a0 = z[e], b0 = z[e + 1];
+            z[e] = a0 * cj - b0 * sj;
+            z[e + 1] = b0 * cj + a0 * sj;
+          } else {
+            const float a0 = x[j], b0 = y[j];
+            x[j] = a0 * cj - b0 * sj;
+            y[j] = b0 * cj + a0 * sj;
           }
         }
       }
-      if (one) {
-        const float* ct = p.cos + line * half + 8 * i;
-        const float* st = p.sin + line * half + 8 * i;
+    }
+    if (!held || (!fits && KIND < 2)) {
+      // no token, or one that the table has no angle for
+      const float fill = held ? __builtin_nanf("") : 0.f;
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          cv[j] = reinterpret_cast<const f32x4*>(ct)[j];
-          sv[j] = reinterpret_cast<const f32x4*>(st)[j];
-        }
+      for (int j = 0; j < 8; ++j) x[j] = y[j] = fill;
+    }
+    if (KIND == 0 || (KIND == 1 && s.out)) {
+      uint16_t* dst = s.out + (size_t)row * D;
+      u32x4 o0, o1;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        o0[j] = T::pack(x[2 * j], x[2 * j + 1]);
+        o1[j] = T::pack(y[2 * j], y[2 * j + 1]);
       }
+      *reinterpret_cast<u32x4*>(dst + c0) = o0;
+      *reinterpret_cast<u32x4*>(dst + c1) = o1;
+    }
+    if (KIND > 0 && s.cache && held && fits && at >= 0 && at < (int64_t)p.table_cols * p.page.d) {
+      const uint32_t n = p.page.div((uint32_t)at);
+      const int page = p.table[(size_t)b * p.table_cols + n];
+      if (page >= 0 && page < p.num_pages) {
+        uint8_t* dst = s.cache + (int64_t)page * p.page_stride +
+                       (int64_t)((uint32_t)at - n * p.page.d) * p.token_stride + (int64_t)h * p.head_stride;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const float cj = cv[j / 4][j % 4], sj = sv[j / 4][j % 4];
-        if (p.interleaved) {
-          float* z = j < 4 ? x : y;
-          const int e = 2 * (j % 4);
-          const float a0 = z[e], b0 = z[e + 1];
-          z[e] = a0 * cj - b0 * sj;
-          z[e + 1] = b0 * cj + a0 * sj;
+        for (int j = 0; j < 8; ++j) x[j] *= s.inv, y[j] *= s.inv;
+        if (p.fp8) {
+          *reinterpret_cast<u32x2*>(dst + c0) = u32x2{pack_fp8(x[0], x[1], x[2], x[3]),
+                                                      pack_fp8(x[4], x[5], x[6], x[7])};
+          *reinterpret_cast<u32x2*>(dst + c1) = u32x2{pack_fp8(y[0], y[1], y[2], y[3]),
+                                                      pack_fp8(y[4], y[5], y[6], y[7])};
         } else {
-          const float a0 = x[j], b0 = y[j];
-          x[j] = a0 * cj - b0 * sj;
-          y[j] = b0 * cj + a0 * sj;
+          u32x4 o0, o1;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            o0[j] = T::pack(x[2 * j], x[2 * j + 1]);
+            o1[j] = T::pack(y[2 * j], y[2 * j + 1]);
+          }
+          *reinterpret_cast<u32x4*>(dst + 2 * c0) = o0;
+          *reinterpret_cast<u32x4*>(dst + 2 * c1) = o1;
         }
       }
     }
-  }
-  if (!held || (!fits && KIND < 2)) {
-    // no token, or one that the table has no angle for
-    const float fill = held ? __builtin_nanf("") : 0.f;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) x[j] = y[j] = fill;
-  }
-  if (KIND == 0 || (KIND == 1 && s.out)) {
-    uint16_t* dst = s.out + (size_t)row * D;
-    u32x4 o0, o1;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      o0[j] = T::pack(x[2 * j], x[2 * j + 1]);
-      o1[j] = T::pack(y[2 * j], y[2 * j + 1]);
-    }
-    *reinterpret_cast<u32x4*>(dst + c0) = o0;
-    *reinterpret_cast<u32x4*>(dst + c1) = o1;
-  }
-  if (KIND > 0 && s.cache && held && fits && at >= 0 && at < (int64_t)p.table_cols * p.page.d) {
-    const uint32_t n = p.page.div((uint32_t)at);
-    const int page = p.table[(size_t)b * p.table_cols + n];
-    if (page >= 0 && page < p.num_pages) {
-      uint8_t* dst = s.cache + (int64_t)page * p.page_stride +
-                     (int64_t)((uint32_t)at - n * p.page.d) * p.token_stride + (int64_t)h * p.head_stride;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) x[j] *= s.inv, y[j] *= s.inv;
-      if (p.fp8) {
-        *reinterpret_cast<u32x2*>(dst + c0) = u32x2{pack_fp8(x[0], x[1], x[2], x[3]),
-                                                    pack_fp8(x[4], x[5], x[6], x[7])};
-        *reinterpret_cast<u32x2*>(dst + c1) = u32x2{pack_fp8(y[0], y[1], y[2], y[3]),
-                                                    pack_fp8(y[4], y[5], y[6], y[7])};
-      } else {
-        u32x4 o0, o1;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          o0[j] = T::pack(x[2 * j], x[2 * j + 1]);
-          o1[j] = T::pack(y[2 * j], y[2 * j + 1]);
-        }
-        *reinterpret_cast<u32x4*>(dst + 2 * c0) = o0;
-        *reinterpret_cast<u32x4*>(dst + 2 * c1) = o1;
-      }
+  };
+  if (HEADS == 1) {
+    one_row(row, h);
+  } else {
+    if (held && turned && fits) load_angles();
+    for (int r = 0; r < HEADS; ++r) {
+      const uint32_t of = h + (p.bnhd ? R : 1) * r;
+      if (of < heads) one_row(p.bnhd ? ((uint32_t)b * p.N + t) * heads + of : (b * heads + of) * p.N + t, of);
     }
   }
 }
 
-template <int DT, int D, bool AXES>
+template <int DT, int D, bool AXES, int HEADS>
 __global__ __launch_bounds__(256) void norm_rope_kernel(Params p) {
   uint32_t unit = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
-  if (unit < p.s[0].units) return unit_rows<DT, D, AXES, 0>(p, p.s[0], unit);
+  if (unit < p.s[0].units) return unit_rows<DT, D, AXES, HEADS, 0>(p, p.s[0], unit);
   unit -= p.s[0].units;
-  if (unit < p.s[1].units) return unit_rows<DT, D, AXES, 1>(p, p.s[1], unit);
+  if (unit < p.s[1].units) return unit_rows<DT, D, AXES, HEADS, 1>(p, p.s[1], unit);
   unit -= p.s[1].units;
-  if (unit < p.s[2].units) unit_rows<DT, D, AXES, 2>(p, p.s[2], unit);
+  if (unit < p.s[2].units) unit_rows<DT, D, AXES, HEADS, 2>(p, p.s[2], unit);
 }
+
+// With positions of several axes a lane takes four heads of its token, so that the angles,
+// which lie in up to eight places of the table for its eight pairs, are fetched once for
+// them (us, one, two, four and eight heads; axes in turn over the pairs: 4 prompts of up to
+// 1999 tokens into E4M3 pages 53.1, 36.9, 32.9, 33.7, 72 heads of 8192 tokens 98.7, 74.5, 63.3,
+// 60.7; a run of pairs each: 28.0, 26.9, 26.9, 28.4 and 60.5, 60.3, 55.5, 54.9).
+constexpr int kHeads = 4;
 
 template <int DT, int D>
 hipError_t launch(const NormRopeArgs& a, hipStream_t stream) {
@@ -279,10 +317,30 @@ hipError_t launch(const NormRopeArgs& a, hipStream_t stream) {
     p.axis_stride = (int64_t)a.B * a.N;
     p.N = a.N, p.used_axes = a.used_axes;
     p.pair_axis[0] = a.pair_axis[0], p.pair_axis[1] = a.pair_axis[1];
-    hipLaunchKernelGGL((norm_rope_kernel<DT, D, true>), dim3((units + 3) / 4), dim3(256), 0, stream, p);
+    // (blocks of rows of one token, or of one head, that would not fill a wavefront, and
+    // launches of few wavefronts, keep one row a lane)
+    const bool blocks = a.layout ? a.Hkv >= kRows && a.H >= kRows : a.N >= kRows;
+    if (blocks && units >= 1024u * kHeads) {
+      units = 0;
+      for (int i = 0; i < 3; ++i) {
+        Stream& s = p.s[i];
+        if (!in[i]) continue;
+        const int heads = i == 0 ? a.H : a.Hkv;
+        const uint32_t token_blocks = (a.N + kRows - 1) / kRows, per = a.layout ? kRows * kHeads : kHeads;
+        const uint32_t head_blocks = (heads + per - 1) / per;
+        s.blocks = FastDiv(a.layout ? head_blocks : token_blocks);
+        s.head_blocks = FastDiv(head_blocks);
+        s.batches = a.B;
+        s.units = (uint32_t)((int64_t)a.B * head_blocks * (a.layout ? a.N : token_blocks));
+        units += s.units;
+      }
+      hipLaunchKernelGGL((norm_rope_kernel<DT, D, true, kHeads>), dim3((units + 3) / 4), dim3(256), 0, stream, p);
+      return hipGetLastError();
+    }
+    hipLaunchKernelGGL((norm_rope_kernel<DT, D, true, 1>), dim3((units + 3) / 4), dim3(256), 0, stream, p);
     return hipGetLastError();
   }
-  hipLaunchKernelGGL((norm_rope_kernel<DT, D, false>), dim3((units + 3) / 4), dim3(256), 0, stream, p);
+  hipLaunchKernelGGL((norm_rope_kernel<DT, D, false, 1>), dim3((units + 3) / 4), dim3(256), 0, stream, p);
   return hipGetLastError();
 }
 

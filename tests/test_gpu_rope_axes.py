@@ -212,6 +212,43 @@ def test_axes_that_no_pair_has_are_not_looked_at(qa):
         assert torch.equal(_bits(a), _bits(b))
 
 
+@pytest.mark.parametrize("layout", ["bnhd", "bhnd"])
+@pytest.mark.parametrize("H,Hkv,d", [(32, 8, 128), (37, 9, 128), (40, 17, 64), (3, 1, 128)])
+def test_large_calls(qa, layout, H, Hkv, d):
+    """Calls in which a lane takes several heads of a token (and those of few heads, in which it
+    does not), odd counts of heads and tokens, padded rows and positions without an angle
+    among them: every element, and every byte of the cache."""
+    import torch
+    B, N, page = 3, 1203, 16
+    q, k, v = _inputs(B, N, H, Hkv, d, torch.bfloat16, layout, 30)
+    cos, sin = so.rotation_table(ROWS, d)
+    axes = _axes_of("any", d // 2, 3)
+    positions = _positions(3, B, N, 31)
+    positions[2, 1, 700] = ROWS
+    counts = torch.tensor([1203, 1000, 5], dtype=torch.int32, device="cuda")
+    starts = torch.tensor([3, 0, 40], dtype=torch.int32, device="cuda")
+    table = torch.randperm(3 * 76, generator=_gen(32), device="cuda").to(torch.int32).view(3, 76)
+    w = (1 + 0.3 * torch.randn(d, generator=_gen(33), device="cuda")).bfloat16()
+    caches = [torch.full((3 * 76, Hkv, page, d), 7.0, device="cuda", dtype=torch.bfloat16) for _ in range(2)]
+    k_out = torch.empty(k.shape, device="cuda", dtype=torch.bfloat16)
+    kw = dict(cos=cos, sin=sin, q_weight=w, k_weight=w, counts=counts, positions=positions, axes=axes, layout=layout)
+    q_out = qa.qk_norm_rope_append(q, k, v, *caches, table, starts, k_out=k_out, **kw)
+    held = (torch.arange(N, device="cuda") < counts[:, None])[:, :, None, None]
+    for x, got in ((q, q_out), (k, k_out)):
+        want, slack = _define(_by_token(x, layout), w, cos, sin, positions, axes, 1e-6, False)
+        so.check_rounded(_by_token(got, layout), torch.where(held, want, 0.0), slack)
+    for a, b in zip(qa.qk_norm_rope(q, k, **kw), (q_out, k_out)):
+        assert torch.equal(_bits(a), _bits(b))
+    want = [torch.full_like(c, 7.0) for c in caches]
+    for b, n in enumerate(counts.tolist()):
+        t = torch.tensor([i for i in range(n) if (b, i) != (1, 700)], device="cuda")
+        at = t + int(starts[b])
+        for c, rows in zip(want, (k_out, v)):
+            c.transpose(1, 2)[table[b, at // page].long(), at % page] = _by_token(rows, layout)[b, t]
+    for c, e in zip(caches, want):
+        assert torch.equal(_bits(c), _bits(e))
+
+
 def test_captured(qa):
     """The axes of the pairs are read at the call; replays follow the positions."""
     import torch
