@@ -462,7 +462,7 @@ int qm_rms_norm(const void* x, const void* residual, const void* weight, void* o
  *
  *   scales       [out] device, fp32, 4-byte aligned: [rows][width / group], or [rows] for
  *                      group = 0.  Each is max |y| / 448 over its columns, at least 2^-126
- *                      (NaN if a y is).  NULL: `scale` is every column's, and nothing is written.
+ *                      (NaN if a y is; where it is not finite, its codes are NaN).  NULL: `scale` is every column's, and nothing is written.
  *   group        columns of a scale: 32, 64, 128, 256, or 0 for the row (QM_ERR_NORM; 0
  *                      without scales).  width is a multiple of it.
  *   scale        without scales: finite, above 0, with a finite reciprocal (QM_ERR_SCALE).

@@ -14,6 +14,10 @@
 // the sum of squares and, for a scale a row, max |s w|, which times 1 / sqrt(..) is max |y|
 // to a rounding.  Maxima are taken of the values' bits without the sign, as whole numbers:
 // a NaN is above every value there, where fmax would drop it.
+//
+// Measured (us; a copy of as many bytes runs at 5.2 TB/s): 8192 rows of 8192 columns, bf16, with
+// a residual 93 (5.8 TB/s); 4097 of 5120, f16 to E4M3 in groups of 128 16.0 (4.0); one row of
+// 4096 2.2, 64 of 8192 to E4M3 with a scale each 4.5: two latencies, of the row and of the sums.
 #include "serving_device.h"
 #include "serving_launch.h"
 
@@ -148,9 +152,9 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void rms_norm_kernel(Params p) {
         *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(p.out) + (int64_t)row * p.width + 8 * at) = o;
     }
   } else {
-    float inv = p.inv;
+    float scale = 1.f, inv = p.inv;
     if (GROUP == 0 && p.scales) {
-      const float scale = scale_of(__builtin_bit_cast(float, top) * r);
+      scale = scale_of(__builtin_bit_cast(float, top) * r);
       if (live && lane == 0) p.scales[row] = scale;
       inv = 1.0f / scale;
     }
@@ -161,16 +165,29 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void rms_norm_kernel(Params p) {
         uint32_t m = 0;
 #pragma unroll
         for (int i = 0; i < 8; ++i) m = magnitude(s[j][i]) > m ? magnitude(s[j][i]) : m;
-        const float scale = scale_of(__builtin_bit_cast(float, max_over<GROUP>(m)));
+        scale = scale_of(__builtin_bit_cast(float, max_over<GROUP>(m)));
         if (live && at < pieces && lane % GROUP == 0)
           p.scales[(int64_t)row * (pieces / GROUP) + at / GROUP] = scale;
         inv = 1.0f / scale;
       }
 #pragma unroll
       for (int i = 0; i < 8; ++i) s[j][i] *= inv;
+      u32x2 codes;
+      if (GROUP > 0 || p.scales) {
+        // at most 448, to a rounding; NaN only where the scale is one, or infinite
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s[j][i] = __builtin_amdgcn_fmed3f(s[j][i], -448.f, 448.f);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          int w = __builtin_amdgcn_cvt_pk_fp8_f32(s[j][4 * i], s[j][4 * i + 1], 0, false);
+          w = __builtin_amdgcn_cvt_pk_fp8_f32(s[j][4 * i + 2], s[j][4 * i + 3], w, true);
+          codes[i] = scale < INFINITY ? (uint32_t)w : 0x7f7f7f7fu;
+        }
+      } else {
+        codes = u32x2{pack_fp8(s[j][0], s[j][1], s[j][2], s[j][3]), pack_fp8(s[j][4], s[j][5], s[j][6], s[j][7])};
+      }
       if (live && at < pieces)
-        *reinterpret_cast<u32x2*>(static_cast<uint8_t*>(p.out) + (int64_t)row * p.width + 8 * at) =
-            u32x2{pack_fp8(s[j][0], s[j][1], s[j][2], s[j][3]), pack_fp8(s[j][4], s[j][5], s[j][6], s[j][7])};
+        *reinterpret_cast<u32x2*>(static_cast<uint8_t*>(p.out) + (int64_t)row * p.width + 8 * at) = codes;
     }
   }
 }
@@ -183,7 +200,10 @@ hipError_t launch(const Params& p, hipStream_t stream) {
   return hipGetLastError();
 }
 
-// The fewest threads that hold a row in four pieces each or fewer.
+// Threads and pieces of a row: four pieces at most, three where they hold it, from 256 threads
+// on.  us, 4097 rows of 5120 columns to E4M3 in groups of 128: 256 threads and three pieces
+// 16.0, and four 18.5, 128 and five 16.3, a wavefront with all 24.5; 4096 rows of 8192 with a
+// residual: 256 threads and four pieces 41.2, 128 and eight 42.9, a wavefront with all 47.5.
 template <int DT, bool FP8, int GROUP>
 hipError_t launch_threads(const Params& p, hipStream_t stream) {
   const int pieces = p.width / 8;
@@ -198,8 +218,11 @@ hipError_t launch_threads(const Params& p, hipStream_t stream) {
   if (pieces <= 128) return launch<DT, 64, 2, FP8, GROUP>(p, stream);
   if (pieces <= 256) return launch<DT, 256, 1, FP8, GROUP>(p, stream);
   if (pieces <= 512) return launch<DT, 256, 2, FP8, GROUP>(p, stream);
-  if (pieces <= 1024) return launch<DT, 256, 4, FP8, GROUP>(p, stream);
-  if (pieces <= 2048) return launch<DT, 512, 4, FP8, GROUP>(p, stream);
+  if (pieces <= 3 * 256) return launch<DT, 256, 3, FP8, GROUP>(p, stream);
+  if (pieces <= 4 * 256) return launch<DT, 256, 4, FP8, GROUP>(p, stream);
+  if (pieces <= 3 * 512) return launch<DT, 512, 3, FP8, GROUP>(p, stream);
+  if (pieces <= 4 * 512) return launch<DT, 512, 4, FP8, GROUP>(p, stream);
+  if (pieces <= 3 * 1024) return launch<DT, 1024, 3, FP8, GROUP>(p, stream);
   return launch<DT, 1024, 4, FP8, GROUP>(p, stream);
 }
 

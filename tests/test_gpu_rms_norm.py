@@ -319,3 +319,20 @@ def test_refusals(qa):
     status(qa.QM_ERR_ALIAS, lambda: qa.rms_norm(x, out=x))
     big = _normal(5, 64, seed=27, dtype=torch.bfloat16)
     status(qa.QM_ERR_ALIAS, lambda: qa.rms_norm(big[:4], residual=x, sum_out=big[1:]))
+
+
+def test_a_scale_that_is_infinite(qa):
+    """A y past fp32 (from an absurd weight): an infinite scale, whose codes are NaN; other
+    groups and rows are not affected."""
+    import torch
+    x = _normal(4, 512, seed=40, dtype=torch.bfloat16)
+    w = torch.ones(512, device="cuda", dtype=torch.bfloat16)
+    w[200] = 3e38
+    x[:, 200] = 1.0
+    x[1, 200] = 300.0   # y = 3e38 * 300 / (root of the mean) overflows here
+    codes, scales, _ = qa.rms_norm_fp8(x, w, group=64)
+    assert torch.isinf(scales[1, 3]) and torch.isnan(codes.float()[1, 192:256]).all()
+    rest = torch.ones(4, 8, dtype=torch.bool, device="cuda")
+    rest[1, 3] = False
+    assert torch.isfinite(scales[rest]).all()
+    assert torch.isfinite(codes.float().view(4, 8, 64)[rest]).all()
