@@ -8,7 +8,9 @@ narrower head than q and k (the MLA shape, 192/128).  ``fwd_fp8`` takes FP8
 [B, N, heads, d] tensors; ``fwd_window`` has a sliding window and visible first keys.
 Around them: ``qk_norm_rope`` makes q and k from a projection's output,
 ``qk_norm_rope_append`` also writes keys and values to a paged cache, and ``decode`` is
-attention of one new token per sequence over that cache.  The
+attention of one new token per sequence over that cache, ``decode_shared`` for sequences that
+share their first tokens.  ``rms_norm`` and ``rms_norm_fp8`` add the residual and normalise
+whole rows between the layers.  The
 operations and their arguments are documented in ``include/qm_attn.h``.
 """
 from .binding import (  # noqa: F401
