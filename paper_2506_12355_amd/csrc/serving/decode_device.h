@@ -15,7 +15,7 @@ namespace {
 
 constexpr int kBlock = kDecodeBlock;   // tokens of a wavefront's step
 constexpr int kMinShare = 4;           // least blocks of a workgroup's share: one a wavefront
-// The second product's factor (see above); O is divided by it at the end.
+// The second product's factor (see decode.hip); O is divided by it at the end.
 template <int DT>
 constexpr float kWeight = DT == 0 ? 32768.f : 1.f;
 // What a row costs a workgroup beside its blocks, in blocks: its first loads and its

@@ -14,7 +14,6 @@ from __future__ import annotations
 
 import ctypes
 import functools
-import operator
 
 from .binding import (QM_BHND, QM_BNHD, QM_OK, QmAttnError, _dtype_code, _enqueue, _int32,
                       _pool_of, load_library, strerror)
@@ -159,19 +158,22 @@ def _cache(k_cache, v_cache, page_table, B, d, dtype, code, index, cache_layout)
     return pages, page_size, heads, columns[1], table, code, layout
 
 
-@functools.lru_cache(maxsize=64)
 def _pair_axes(axes, pairs, count):
     """The library's array of each pair's axis."""
     if axes is None:
         if count != 1:
             raise ValueError("axes must name each rotated pair's axis where positions has several")
         return bytes(pairs)
+    axes = tuple(axes)
     if len(axes) != pairs:
         raise ValueError(f"axes must name the axis of each of the {pairs} rotated pairs, not of {len(axes)}")
-    axes = [operator.index(a) for a in axes]
-    if not all(0 <= a < count for a in axes):
+    try:
+        own = bytes(axes)
+    except ValueError:   # one of them below 0 or above 255
+        own = None
+    if own is None or (own and max(own) >= count):
         raise ValueError(f"axes must be from 0 to {count - 1}, positions' axes")
-    return bytes(axes)
+    return own
 
 
 def _positions(positions, axes, rotary, B, N, index):
@@ -180,7 +182,7 @@ def _positions(positions, axes, rotary, B, N, index):
     if len(size) != 3 or not 1 <= size[0] <= 4:
         raise ValueError("positions must have shape [axes, B, N] with 1 to 4 axes")
     at = _vector("positions", positions, (size[0], B, N), index, _torch().int32)
-    return at, _pair_axes(axes if axes is None else tuple(axes), rotary // 2, size[0]), size[0]
+    return at, _pair_axes(axes, rotary // 2, size[0]), size[0]
 
 
 def qk_norm_rope(q, k, cos=None, sin=None, q_weight=None, k_weight=None, eps: float = 1e-6,

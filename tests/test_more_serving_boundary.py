@@ -182,3 +182,22 @@ def test_host_tensors_are_refused():
     for call in (lambda: qa.rms_norm(x), lambda: qa.rms_norm_fp8(x)):
         with pytest.raises(ValueError, match="ROCm device"):
             call()
+
+
+def test_axes_are_read_in_each_call():
+    """Whole numbers of any kind, as they stand when a call is made."""
+    import numpy as np
+    import torch
+    from paper_2506_12355_amd.serving import _pair_axes
+    held = torch.tensor([0, 1, 2, 2])
+    own = tuple(held)
+    assert _pair_axes(own, 4, 3) == bytes([0, 1, 2, 2])
+    held[0] = 2
+    assert _pair_axes(own, 4, 3) == bytes([2, 1, 2, 2])
+    assert _pair_axes(np.array([1, 0], dtype=np.int64), 2, 2) == bytes([1, 0])
+    assert _pair_axes((1, 0), 2, 2) == bytes([1, 0])
+    with pytest.raises(TypeError):
+        _pair_axes((1.0, 0.0), 2, 2)
+    for axes in ((0, 2), (0, -1), (0, 256), (0, 1, 1), ()):
+        with pytest.raises(ValueError, match="axes must"):
+            _pair_axes(axes, 2, 2)
