@@ -298,19 +298,6 @@ int plan(int B, int H, int Hkv, int d, int page_size, int table_cols, int max_le
   return QM_OK;
 }
 
-// The same for a call behind a shared prefix of at least one token.
-int plan_shared(int B, int H, int Hkv, int d, int page_size, int table_cols, int prefix,
-                int max_length, qm::SharedPlan* p, int* limit) {
-  qm::DecodePlan unused;
-  const int st = plan(B, H, Hkv, d, page_size, table_cols, max_length, 0, 0, &unused, limit);
-  if (st != QM_OK) return st;
-  // the longest a sequence can be; its own pages may end before the prefix does
-  if (prefix < 1 || prefix > kMostTokens || prefix > max_length) return QM_ERR_PAGE;
-  if (*limit < prefix) *limit = prefix;
-  *p = qm::plan_shared(B, H, Hkv, *limit, prefix, device_cus());
-  return QM_OK;
-}
-
 // Two partial results of 16 heads for each workgroup of a call in shares, and two
 // numbers for each row.
 size_t workspace_of(const qm::DecodePlan& p, int B, int H, int Hkv, int d) {
@@ -324,6 +311,25 @@ size_t workspace_of(const qm::SharedPlan& p, int B, int H, int Hkv, int d) {
   const size_t slots = (size_t)Hkv * p.tiles * p.rt * p.splits + qm::own_slots(p, B, H, Hkv);
   const size_t rows = p.own_grid ? (size_t)B * Hkv * ((H / Hkv + 15) / 16) : 0;
   return slots * 16 * (d + 2) * sizeof(float) + rows * 2 * sizeof(int32_t);
+}
+
+// The same for a call behind a shared prefix of at least one token, of a cache of es bytes a
+// value; its workspace serves either type's, as qm_attn_decode_shared_workspace knows none.
+int plan_shared(int B, int H, int Hkv, int d, int es, int page_size, int table_cols, int prefix,
+                int max_length, qm::SharedPlan* p, int* limit, size_t* bytes) {
+  qm::DecodePlan unused;
+  const int st = plan(B, H, Hkv, d, page_size, table_cols, max_length, 0, 0, &unused, limit);
+  if (st != QM_OK) return st;
+  // the longest a sequence can be; its own pages may end before the prefix does
+  if (prefix < 1 || prefix > kMostTokens || prefix > max_length) return QM_ERR_PAGE;
+  if (*limit < prefix) *limit = prefix;
+  const int cus = device_cus();
+  const qm::SharedPlan codes = qm::plan_shared(B, H, Hkv, d, 1, *limit, prefix, cus);
+  const qm::SharedPlan values = qm::plan_shared(B, H, Hkv, d, 2, *limit, prefix, cus);
+  *p = es == 1 ? codes : values;
+  const size_t x = workspace_of(codes, B, H, Hkv, d), y = workspace_of(values, B, H, Hkv, d);
+  *bytes = x > y ? x : y;
+  return QM_OK;
 }
 
 // Both entry points; shared: the one with a prefix of `prefix` tokens in prefix_table.
@@ -365,10 +371,12 @@ int decode(const void* q, const void* k_cache, const void* v_cache, void* o, flo
     return QM_ERR_UNSUPPORTED;
   qm::DecodePlan p;
   qm::SharedPlan s;
-  st = prefix ? plan_shared(B, H, Hkv, d, page_size, table_cols, prefix, max_length, &s, &a.limit)
+  size_t need = 0;
+  st = prefix ? plan_shared(B, H, Hkv, d, a.cache.fp8 ? 1 : 2, page_size, table_cols, prefix, max_length, &s,
+                            &a.limit, &need)
               : plan(B, H, Hkv, d, page_size, table_cols, max_length, window, sinks, &p, &a.limit);
   if (st != QM_OK) return st;
-  const size_t need = prefix ? workspace_of(s, B, H, Hkv, d) : workspace_of(p, B, H, Hkv, d);
+  if (!prefix) need = workspace_of(p, B, H, Hkv, d);
   if (need) {
     if (!workspace || workspace_bytes < need) return QM_ERR_WORKSPACE;
     const Range rw = {workspace, need};
@@ -503,8 +511,9 @@ extern "C" int qm_attn_decode_shared_workspace(int B, int H, int Hkv, int d, int
     return qm_attn_decode_workspace(B, H, Hkv, d, page_size, table_cols, max_length, 0, 0, bytes);
   qm::SharedPlan p;
   int limit;
-  const int st = plan_shared(B, H, Hkv, d, page_size, table_cols, prefix_length, max_length, &p, &limit);
-  if (st == QM_OK) *bytes = workspace_of(p, B, H, Hkv, d);
+  size_t need;
+  const int st = plan_shared(B, H, Hkv, d, 2, page_size, table_cols, prefix_length, max_length, &p, &limit, &need);
+  if (st == QM_OK) *bytes = need;
   return st;
 }
 

@@ -12,8 +12,9 @@ from paper_2506_12355_amd import build as qbuild
 
 WRAPPER = """
 #include "serving/shared_rules.h"
-extern "C" void plan(long long B, long long H, long long Hkv, long long limit, long long prefix, int cus, int* out) {
-  const qm::SharedPlan p = qm::plan_shared(B, H, Hkv, limit, prefix, cus);
+extern "C" void plan(long long B, long long H, long long Hkv, int d, int es, long long limit, long long prefix, int cus,
+                     int* out) {
+  const qm::SharedPlan p = qm::plan_shared(B, H, Hkv, d, es, limit, prefix, cus);
   out[0] = p.rt, out[1] = p.tiles, out[2] = p.splits, out[3] = p.prefix_grid, out[4] = p.own_grid, out[5] = p.join_threads;
 }
 """
@@ -32,11 +33,11 @@ def plan(tmp_path_factory):
     subprocess.run([cc, "-x", "hip", "--cuda-host-only", "--offload-arch=gfx950", "-O1", "-std=c++17", "-fPIC",
                     "-shared", "-I", qbuild.CSRC, "-o", so, src], check=True, capture_output=True)
     lib = ctypes.CDLL(so)
-    lib.plan.argtypes = [ctypes.c_longlong] * 5 + [ctypes.c_int, ctypes.c_void_p]
+    lib.plan.argtypes = [ctypes.c_longlong] * 3 + [ctypes.c_int] * 2 + [ctypes.c_longlong] * 2 + [ctypes.c_int, ctypes.c_void_p]
 
-    def call(B, H, Hkv, limit, prefix, cus=256):
+    def call(B, H, Hkv, limit, prefix, cus=256, d=128, es=2):
         out = (ctypes.c_int * 6)()
-        lib.plan(B, H, Hkv, limit, prefix, cus, out)
+        lib.plan(B, H, Hkv, d, es, limit, prefix, cus, out)
         return dict(zip(("rt", "tiles", "splits", "prefix_grid", "own_grid", "join_threads"), out))
     return call
 
@@ -83,3 +84,19 @@ def test_own_shares(plan):
 def test_threads_of_the_join(plan):
     assert plan(32, 32, 8, 500, 500)["join_threads"] == 64
     assert plan(31, 32, 8, 500, 500)["join_threads"] == 256
+
+
+@pytest.mark.parametrize("prefix,more,d,es,parts", [
+    # 64 sequences of 64/8 heads, 32 tiles: 8 parts are a workgroup a CU, 16 two
+    (8192, 0, 128, 2, 16), (8192, 64, 128, 2, 8), (8192, 8000, 128, 2, 8), (32768, 64, 128, 2, 16),
+    (32768, 8000, 128, 2, 8), (32768, 2000, 128, 1, 16), (32768, 8000, 128, 1, 8), (8192, 2000, 64, 2, 8),
+    (32768, 2000, 64, 2, 16),
+])
+def test_a_workgroup_of_each_a_cu(plan, prefix, more, d, es, parts):
+    """Where own tokens are read beside the prefix's products its parts are one a CU."""
+    assert plan(64, 64, 8, prefix + more, prefix, d=d, es=es)["splits"] == parts
+
+
+def test_rows_that_wait_for_memory_take_two(plan):
+    for more in (0, 500, 8000):
+        assert plan(8, 64, 8, 16384 + more, 16384)["splits"] == 32   # of 16 tiles
