@@ -27,14 +27,15 @@ inline SharedPlan plan_shared(int64_t B, int64_t H, int64_t Hkv, int d, int es, 
   // a third slower; but the prefix alone takes a quarter longer with one workgroup a CU than with
   // two.  So one, where the prefix's work is at most four times what own tokens then cost nothing
   // and what half as many parts save, in units of a block of 128 rows (2.7 ns at d = 128; so much
-  // is a block of own tokens of 16 KB; of their most, half is counted, as lengths vary).
+  // is a block of own tokens of 16 KB; of their most, half is counted, as lengths vary).  Few
+  // rows, which wait for memory, take one by the same rule, a tile's block as half a unit.
   // us, both ways, 64/8 heads, the prefix's tokens and the most own ones: 64 sequences
   // 8192 + 64 53.6, 47.9, + 500 58.2, 49.3, + 8000 241, 211; 32768 + 64 120, 127, + 8000 289, 229;
   // of E4M3 32768 + 2000 136, 142, + 8000 210, 173; d = 64 8192 + 2000 46.3, 37.8, 32768 + 2000 83.8,
-  // 94.8.
-  const double prefix_work = (double)(Hkv * tiles * blocks) * (d == 128 ? 1.0 : 0.65);
+  // 94.8; 8 sequences 16384 + 300 31.0, 24.1, 65536 + 300 66.4, 68.9, d = 64 35.8, 44.9.
+  const double prefix_work = (double)(Hkv * tiles * blocks) * (p.rt == 8 ? 1.0 : 0.5) * (d == 128 ? 1.0 : 0.65);
   const double own_work = (double)(own_rows * own_blocks) * (d * es / 256.0), saved = 7600.0 * d / 128;
-  const bool beside = p.rt == 8 && own_blocks && prefix_work < own_work + saved;
+  const bool beside = own_blocks && prefix_work < own_work + saved;
   const int64_t slots = (beside ? 1 : 2) * (int64_t)cus;
   // Parts that fill one to four rounds of the workgroups that are on the device at once, or one
   // part a tile: the rounds' blocks, and what a part costs beside them.
@@ -52,7 +53,12 @@ inline SharedPlan plan_shared(int64_t B, int64_t H, int64_t Hkv, int d, int es, 
   p.prefix_grid = (int)((Hkv * splits + 7) / 8 * 8 * tiles);
   const int64_t shares = (own_rows * (own_blocks + 6) + 3) / 4;
   p.join_threads = B * H < 4 * (int64_t)cus ? 256 : 64;
-  p.own_grid = own_blocks ? (int)(shares < 2 * cus ? shares : 2 * cus) : 0;
+  // Beside few rows, own tokens' workgroups are those that are on the device with the prefix's, one a
+  // CU at least (us, and with two a CU: 8 sequences 4000 + 1000 17.5, 21.6, + 4000 22.4, 27.2).  Beside
+  // many, whose workgroups end first where own tokens are many, two (d = 64 and E4M3 up to 30%
+  // faster, else 2-4% slower).
+  const int64_t left = 2 * (int64_t)cus - (p.rt == 8 ? 0 : p.prefix_grid), grid = left < cus ? cus : left;
+  p.own_grid = own_blocks ? (int)(shares < grid ? shares : grid) : 0;
   return p;
 }
 

@@ -97,6 +97,12 @@ def test_a_workgroup_of_each_a_cu(plan, prefix, more, d, es, parts):
     assert plan(64, 64, 8, prefix + more, prefix, d=d, es=es)["splits"] == parts
 
 
-def test_rows_that_wait_for_memory_take_two(plan):
-    for more in (0, 500, 8000):
-        assert plan(8, 64, 8, 16384 + more, 16384)["splits"] == 32   # of 16 tiles
+@pytest.mark.parametrize("prefix,more,d,parts,own", [
+    # 8 sequences of 64/8 heads, 16 tiles of 32 rows
+    (16384, 0, 128, 32, 0), (16384, 500, 128, 16, 256), (65536, 500, 128, 32, 256), (65536, 500, 64, 32, 256),
+    (1000, 500, 128, 4, 352), (4000, 4000, 128, 16, 256),
+])
+def test_few_rows(plan, prefix, more, d, parts, own):
+    """The same rule; own tokens' workgroups are those for which the prefix's leave room."""
+    p = plan(8, 64, 8, prefix + more, prefix, d=d)
+    assert (p["splits"], p["own_grid"]) == (parts, own)
