@@ -543,7 +543,8 @@ int qm_attn_decode_workspace(int B, int H, int Hkv, int d, int page_size, int ta
  *                      table, or a page out of range among the sequence's: that sequence's
  *                      o and lse are NaN (with a page of the prefix every sequence's of a
  *                      length above 0).
- *   max_length   prefix_length or more (QM_ERR_PAGE).
+ *   max_length   prefix_length or more (QM_ERR_PAGE).  With prefix_length it decides how the work is
+ *                divided: one far above the longest sequence costs up to a quarter of the time.
  *   workspace    of qm_attn_decode_shared_workspace bytes.
  *   All other arguments, the arithmetic and the status codes are those of qm_attn_decode.
  *   Two kernels are enqueued.

@@ -583,7 +583,8 @@ def decode_shared(q, k_cache, v_cache, page_table, lengths, prefix_table, prefix
     Returns (o [B, H, d], lse float32 [B, H]).  Length 0 (a free slot) gives o = 0 and lse
     = -inf; any other length below ``prefix_length`` gives NaN, as do the lengths and page
     numbers out of range that do for ``decode`` (a page of the prefix for every sequence).
-    ``workspace``: as for ``decode``, of :func:`decode_shared_workspace` bytes.  For
+    ``max_length``, also where the page table could hold more, tells how the work is best
+    divided.  ``workspace``: as for ``decode``, of :func:`decode_shared_workspace` bytes.  For
     layers with a window call ``decode``, with the prefix's pages in each sequence's row.
     (``qm_attn_decode_shared``)"""
     return _decode(q, k_cache, v_cache, page_table, lengths, scale, k_scale, v_scale, max_length, out, lse,
