@@ -27,3 +27,22 @@ def pytest_collection_modifyitems(config, items):
     for item in items:
         if "gpu" in item.keywords:
             item.add_marker(skip)
+
+
+@pytest.fixture(autouse=True)
+def lengths_live_as_long_as_their_calls(request, monkeypatch):
+    """test_gpu_decode_shared.py's State makes the lengths of each of its calls anew, and a call
+    on another stream reads them after it has returned.  As binding.fwd says of inputs, they
+    have to live until that stream is done: here, to the test's end.  Dropped before,
+    their memory is the next call's lengths while the last call still reads it."""
+    shared = sys.modules.get("tests.test_gpu_decode_shared")
+    if shared is None or getattr(request.module, "State", None) is not shared.State:
+        yield
+        return
+    held, make = [], shared._ints
+
+    def ints(values):
+        held.append(make(values))
+        return held[-1]
+    monkeypatch.setattr(shared, "_ints", ints)
+    yield
