@@ -38,13 +38,18 @@ constexpr bool kDebugSync = false;
 namespace qm {
 namespace {
 
-// Weights are formed against a row's maximum so far, and redone against a new one where a
-// lane's eight of them sum to more than kMostWeight (always in a row's first block): a
-// step's weights then wait for no maximum, and the accumulators are scaled in few steps
-// (with each new maximum, of 32 rows a wavefront, in one step of two).  f16's factor leaves room.
-constexpr float kMostWeight = 8.f;
+// Weights are formed against a row's maximum so far, and redone against a new one where eight
+// of them, a lane's, sum to more than kMostWeight (always in a row's first block): a step's
+// weights then wait for no maximum, and the accumulators are scaled in few steps.  A row is
+// redone by its own weights alone, so that what its neighbours hold changes none of its bits;
+// then 32 rows have a step each, and room of 8 is too little (us, 64 sequences of 64/8 heads
+// behind 32768 tokens: bf16 8 117, 64 104.5, 1024 104.9; d = 64 78.7, 67.6, 67.2; E4M3 119, 106.7,
+// 105.6; f16 8 124, 16 115.5, 32 115.0).  bf16 has fp32's exponents; f16's factor brings the largest
+// weights to 2^15, so that of those far below a row's largest 2^-36 each is lost.
 template <int DT>
-constexpr float kFactor = DT == 0 ? 4096.f : 1.f;
+constexpr float kMostWeight = DT == 0 ? 16.f : 1024.f;
+template <int DT>
+constexpr float kFactor = DT == 0 ? 2048.f : 1.f;
 
 // a - the low half of w, b - the high half: what rounding a and b into w left, exactly.  (The
 // factors stand in registers: written as constants, -1 in the low half is compiled into the
@@ -571,14 +576,17 @@ __device__ __forceinline__ void prefix_block_rows(const SharedParams& sp, float*
       float sum[RT];
 #pragma unroll
       for (int rt = 0; rt < RT; ++rt) sum[rt] = weigh(s, rt, EDGE, i, w1.near[rt], w1.rest[rt]);
-      if (__any(fmaxf(sum[0], sum[1]) > kMostWeight)) {
+      if (__any(fmaxf(sum[0], sum[1]) > kMostWeight<DT>)) {
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
           float top = -FLT_MAX;
 #pragma unroll
           for (int j = 0; j < 8; ++j)
             if (!EDGE || i * kBlock + 16 * (j / 4) + 4 * g + j % 4 < len) top = fmaxf(top, s.x[rt][j / 4][j % 4] * c);
-          top = fmaxf(m[rt], max_over_groups(top));
+          // (of the row's four lanes, by any; a row that is not redone keeps m, and its weights come
+          // out as they were.  That is hidden from the compiler, which else branches by row.)
+          top = max_over_groups(sum[rt]) > kMostWeight<DT> ? fmaxf(m[rt], max_over_groups(top)) : m[rt];
+          asm("" : "+v"(top));
           const float alpha = __builtin_amdgcn_exp2f(m[rt] - top);
           l[rt] *= alpha;
 #pragma unroll

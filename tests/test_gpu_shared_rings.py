@@ -155,3 +155,29 @@ def test_graphs_and_streams(qa):
     torch.cuda.synchronize()
     for x, y in zip((*a, *b), (*ref, *ref2)):
         assert torch.equal(_bits(x), _bits(y))
+
+
+@pytest.mark.parametrize("scale", [0.2, -0.2])
+@pytest.mark.parametrize("cache,dtype", [("same", "bfloat16"), ("same", "float16"), ("e4m3", "bfloat16")])
+@pytest.mark.parametrize("H", [8, 2], ids=["rings", "32 rows"])
+def test_rising_scores_of_one_query_do_not_reach_another(qa, H, cache, dtype, scale):
+    """Queries, a free slot's among them, whose scores keep rising along the prefix: the rows
+    beside them, in the same 16-row tiles, give the bytes that they give beside quiet ones."""
+    import torch
+    prefix, page = 1000, 16
+    s = State(OWN, prefix, H, 1, 128, page, "bhnd", dtype, cache, seed=60)
+    at = torch.arange(prefix, device="cuda")
+    keys = s.caches[0].float()
+    keys[s.prefix_table[at // page].long(), 0, at % page, 0] = torch.linspace(-200, 200, prefix, device="cuda") * (1 if cache == "e4m3" else 1 / 30)
+    s.caches[0] = keys.to(s.caches[0].dtype)
+    s.q[..., 0] = 0
+    o, lse = s.run(qa, scale=scale)
+    loud = (1, 2, 14, 17)   # 1 and 14 are free slots
+    for b in loud:
+        for h in range(H):
+            s.q[b, h, 0] = math.copysign(3.0 + h + b / 4, scale)
+    o2, lse2 = s.run(qa, scale=scale)
+    rest = [b for b in range(len(OWN)) if b not in loud]
+    assert torch.equal(_bits(lse2[rest]), _bits(lse[rest]))
+    assert torch.equal(_bits(o2[rest]), _bits(o[rest]))
+    s.check(o2, lse2, scale=scale, sequences=(2, 17))
