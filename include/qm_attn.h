@@ -449,7 +449,8 @@ int qm_qk_norm_rope_append_axes(
  *   width        a multiple of 8 from 8 to 32768 (QM_ERR_NORM).     rows   1 or more.
  *   A row whose mean square overflows fp32 has y = 0; one that holds a NaN or an infinity
  *   has NaN in y, there at least.  Other rows are not affected.
- *   stream, errors, capture: as for the calls above (one kernel, nothing else).
+ *   stream, errors, capture: as for the calls above (one kernel, or, of more than 2^21 rows,
+ *   one for each 2^21 at least; nothing else).
  */
 int qm_rms_norm(const void* x, const void* residual, const void* weight, void* out, void* sum,
                 int rows, int width, long long x_stride, long long residual_stride,

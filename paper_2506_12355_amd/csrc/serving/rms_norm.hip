@@ -18,6 +18,7 @@
 // Measured (us; a copy of as many bytes runs at 5.2 TB/s): 8192 rows of 8192 columns, bf16, with
 // a residual 93 (5.8 TB/s); 4097 of 5120, f16 to E4M3 in groups of 128 16.0 (4.0); one row of
 // 4096 2.2, 64 of 8192 to E4M3 with a scale each 4.5: two latencies, of the row and of the sums.
+#include "norm_rules.h"
 #include "serving_device.h"
 #include "serving_launch.h"
 
@@ -195,9 +196,21 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void rms_norm_kernel(Params p) {
 template <int DT, int T, int V, bool FP8, int GROUP>
 hipError_t launch(const Params& p, hipStream_t stream) {
   constexpr int kRows = T < 256 ? 256 / T : 1;
-  hipLaunchKernelGGL((rms_norm_kernel<DT, T, V, FP8, GROUP>), dim3((p.rows + kRows - 1) / kRows),
-                     dim3(T < 256 ? 256 : T), 0, stream, p);
-  return hipGetLastError();
+  Params part = p;
+  for (int64_t first = 0; first < p.rows; first += rows_of_launch(T)) {
+    const int64_t left = p.rows - first;
+    part.rows = (int)(left < rows_of_launch(T) ? left : rows_of_launch(T));
+    part.x = p.x + first * p.x_stride;
+    if (p.residual) part.residual = p.residual + first * p.residual_stride;
+    if (p.sum) part.sum = p.sum + first * p.sum_stride;
+    part.out = static_cast<uint8_t*>(p.out) + first * p.width * (FP8 ? 1 : 2);
+    if (p.scales) part.scales = p.scales + first * (GROUP ? p.width / (8 * GROUP) : 1);
+    hipLaunchKernelGGL((rms_norm_kernel<DT, T, V, FP8, GROUP>), dim3((part.rows + kRows - 1) / kRows),
+                       dim3(T < 256 ? 256 : T), 0, stream, part);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 // Threads and pieces of a row: four pieces at most, three where they hold it, from 256 threads

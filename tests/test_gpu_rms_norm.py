@@ -336,3 +336,34 @@ def test_a_scale_that_is_infinite(qa):
     rest[1, 3] = False
     assert torch.isfinite(scales[rest]).all()
     assert torch.isfinite(codes.float().view(4, 8, 64)[rest]).all()
+
+
+@pytest.mark.parametrize("width,rows,launch", [(1056, (1 << 24) + 70, 1 << 23), (8, (1 << 29) + 3, 1 << 28)])
+def test_more_rows_than_one_launch_takes(qa, width, rows, launch):
+    """Rows of 2^32 threads and more: those on either side of each launch's end, and some from
+    everywhere, as in a call of their own, and every row written."""
+    import torch
+    # rows that begin 8 elements apart
+    x = torch.empty(rows * 8 + width, device="cuda", dtype=torch.bfloat16).normal_(generator=_gen(43)).as_strided((rows, width), (8, 1))
+    w = _normal(width, seed=44, dtype=torch.bfloat16)
+    at = torch.cat([torch.arange(max(0, e - 40), min(rows, e + 40)) for e in [0, *range(launch, rows, launch), rows]]
+                   + [torch.randint(0, rows, (2000,), generator=torch.Generator().manual_seed(45))]).cuda()
+    some = x[at].contiguous()
+    if width == 8:
+        y, _ = qa.rms_norm(x, w, out=torch.full((rows, width), 99.0, device="cuda", dtype=torch.bfloat16))
+        assert torch.equal(_bits(y[at]), _bits(qa.rms_norm(some, w)[0]))
+        for lo in range(0, rows, 1 << 27):   # (no y of 8 columns reaches 99)
+            assert not (y[lo:lo + (1 << 27)] == 99).any()
+        return
+    r = _normal(1, width, seed=46, dtype=torch.bfloat16)
+    scales = torch.full((rows, 1), -1.0, device="cuda")
+    codes, _, total = qa.rms_norm_fp8(x, w, residual=r.expand(rows, width), scales=scales)
+    ref = qa.rms_norm_fp8(some, w, residual=r.expand(at.numel(), width))
+    for a, b in zip((codes.view(torch.uint8), scales, total), ref):
+        assert torch.equal(_bits(a[at]), _bits(b))
+    assert (scales > 0).all()
+    groups = torch.full((rows, 33), -1.0, device="cuda")
+    qa.rms_norm_fp8(x, group=32, out=codes, scales=groups)
+    ref = qa.rms_norm_fp8(some, group=32)
+    assert torch.equal(_bits(codes.view(torch.uint8)[at]), _bits(ref[0])) and torch.equal(groups[at], ref[1])
+    assert (groups > 0).all()
