@@ -11,9 +11,10 @@
 // Bound: memory; each element is read and written once.  A row belongs to T threads, each
 // with V pieces of 8 columns that stay in registers from the one read to the last write: a
 // part of a wavefront (T = 8 to 64, several rows a wavefront), or a workgroup.  One exchange:
-// the sum of squares and, for a scale a row, max |s w|, which times 1 / sqrt(..) is max |y|
-// to a rounding.  Maxima are taken of the values' bits without the sign, as whole numbers:
-// a NaN is above every value there, where fmax would drop it.
+// the sum of squares and, for a scale a row, max |s w|, which times 1 / sqrt(..) is max |y| to
+// a rounding; rows whose products leave fp32's range, where y need not, take a second one, of
+// y.  Maxima are taken of the values' bits without the sign, as whole numbers: a NaN is above
+// every value there, where fmax would drop it.
 //
 // Measured (us; a copy of as many bytes runs at 5.2 TB/s): 8192 rows of 8192 columns, bf16, with
 // a residual 93 (5.8 TB/s); 4097 of 5120, f16 to E4M3 in groups of 128 16.0 (4.0); one row of
@@ -47,6 +48,8 @@ __device__ __forceinline__ uint32_t max_over(uint32_t x) {
 __device__ __forceinline__ uint32_t magnitude(float x) {
   return __builtin_bit_cast(uint32_t, x) & 0x7fffffffu;
 }
+
+constexpr uint32_t kInfinite = 0x7f800000u, kLeastProduct = 0x0d800000u;   // bits of infinity and of 2^-100
 
 // The scale of values up to m in magnitude: at least 2^-126, whose reciprocal is finite;
 // NaN stays.
@@ -116,9 +119,9 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void rms_norm_kernel(Params p) {
   }
   squares = sum_over<(T < 64 ? T : 64)>(squares);
   if (FP8 && GROUP == 0) top = max_over<(T < 64 ? T : 64)>(top);
+  __shared__ uint32_t tops[kWaves > 1 ? kWaves : 1];
   if constexpr (kWaves > 1) {
     __shared__ float parts[kWaves];
-    __shared__ uint32_t tops[kWaves];
     if (threadIdx.x % 64 == 0) {
       parts[threadIdx.x / 64] = squares;
       if (FP8 && GROUP == 0) tops[threadIdx.x / 64] = top;
@@ -155,7 +158,27 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void rms_norm_kernel(Params p) {
   } else {
     float scale = 1.f, inv = p.inv;
     if (GROUP == 0 && p.scales) {
-      scale = scale_of(__builtin_bit_cast(float, top) * r);
+      float most = __builtin_bit_cast(float, top) * r;
+      // where the largest |s w| is past fp32's range, or so small that it lost bits, y need not be
+      const bool lost = top - kLeastProduct >= kInfinite - kLeastProduct;
+      if (__any(lost)) {   // (more than one wavefront: of all of them)
+        uint32_t formed = 0;
+#pragma unroll
+        for (int j = 0; j < V; ++j)
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            if (j * T + lane < pieces && magnitude(s[j][i]) > formed) formed = magnitude(s[j][i]);
+        formed = max_over<(T < 64 ? T : 64)>(formed);
+        if constexpr (kWaves > 1) {
+          __syncthreads();   // (tops has been read)
+          if (threadIdx.x % 64 == 0) tops[threadIdx.x / 64] = formed;
+          __syncthreads();
+#pragma unroll
+          for (int i = 0; i < kWaves; ++i) formed = tops[i] > formed ? tops[i] : formed;
+        }
+        if (lost) most = __builtin_bit_cast(float, formed);
+      }
+      scale = scale_of(most);
       if (live && lane == 0) p.scales[row] = scale;
       inv = 1.0f / scale;
     }

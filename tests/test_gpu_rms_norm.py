@@ -338,6 +338,45 @@ def test_a_scale_that_is_infinite(qa):
     assert torch.isfinite(codes.float().view(4, 8, 64)[rest]).all()
 
 
+@pytest.mark.parametrize("width", [64, 128, 256, 512, 1024, 4096, 16384, 32768])
+def test_products_beyond_fp32_where_the_result_is_not(qa, width):
+    """|s w| past fp32's range, or below it, in rows whose y is neither: a scale a row is that
+    of the y that are formed, as a scale a group is, and the rows beside them keep their bytes."""
+    import torch
+    def inputs(s, w):
+        x = _normal(9, width, seed=41, dtype=torch.bfloat16)
+        x[2] *= s
+        x[7] *= s
+        return x, (_normal(width, seed=42, dtype=torch.float32) * w).bfloat16()
+
+    # a mean square past fp32: y is 0, whatever the weight
+    x, w = inputs(1.0, 1.0)
+    x[2], x[7] = 3e38, -3e38
+    w[:] = 1.5
+    ref, ref_scales, _ = qa.rms_norm_fp8(x[:2], w)
+    for kw in (dict(), dict(group=32), dict(scale=0.02)):
+        codes, scales, _ = qa.rms_norm_fp8(x, w, **kw)
+        assert (codes.float()[[2, 7]] == 0).all(), kw
+        if scales is not None:
+            assert (scales[[2, 7]] == 2.0 ** -126).all(), kw
+        if not kw:
+            assert torch.equal(_bits(codes[:2]), _bits(ref)) and torch.equal(scales[:2], ref_scales)
+    # s w overflows (below: is lost), y does not
+    for s, w, eps in ((1e12, 1e30, 1e-6), (1e-15, 1e-30, 0.0)):
+        x, w = inputs(s, w)
+        y, _ = _define(x, w, None, eps)
+        assert torch.isfinite(y.float()).all() and (y.abs().amax(-1) > 1e-35).all()
+        for group in (None, 32):
+            codes, scales, _ = qa.rms_norm_fp8(x, w, eps=eps, group=group)
+            _check_codes(codes, scales, y, group or 0, f"{s} {group}")
+        quiet = x.clone()
+        quiet[2], quiet[7] = 1.0, 1.0
+        codes, scales, _ = qa.rms_norm_fp8(x, w, eps=eps)
+        ref, ref_scales, _ = qa.rms_norm_fp8(quiet, w, eps=eps)
+        rest = [0, 1, 3, 4, 5, 6, 8]
+        assert torch.equal(_bits(codes[rest]), _bits(ref[rest])) and torch.equal(scales[rest], ref_scales[rest])
+
+
 @pytest.mark.parametrize("width,rows,launch", [(1056, (1 << 24) + 70, 1 << 23), (8, (1 << 29) + 3, 1 << 28)])
 def test_more_rows_than_one_launch_takes(qa, width, rows, launch):
     """Rows of 2^32 threads and more: those on either side of each launch's end, and some from
