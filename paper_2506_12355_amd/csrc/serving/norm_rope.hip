@@ -192,6 +192,9 @@ __device__ __forceinline__ void unit_rows(const Params& p, const Stream& s, uint
       }
       if (turned && fits) {
         if (HEADS == 1) load_angles();
+        // Which product is rounded before the sum is said here, not left to the compiler, so that
+        // every instance gives the same bytes.  (In interleaved pairs 4 to 6 of a lane the other one
+        // is, in b cos + a sin: the bytes that calls of one axis gave while it was left.)
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
           const float cj = cv[j / 4][j % 4], sj = sv[j / 4][j % 4];
@@ -199,12 +202,12 @@ __device__ __forceinline__ void unit_rows(const Params& p, const Stream& s, uint
             float* z = j < 4 ? x : y;
             const int e = 2 * (j % 4);
             const float a0 = z[e], b0 = z[e + 1];
-            z[e] = a0 * cj - b0 * sj;
-            z[e + 1] = b0 * cj + a0 * sj;
+            z[e] = fmaf(a0, cj, -(b0 * sj));
+            z[e + 1] = j < 4 || j == 7 ? fmaf(b0, cj, a0 * sj) : fmaf(a0, sj, b0 * cj);
           } else {
             const float a0 = x[j], b0 = y[j];
-            x[j] = a0 * cj - b0 * sj;
-            y[j] = b0 * cj + a0 * sj;
+            x[j] = fmaf(a0, cj, -(b0 * sj));
+            y[j] = fmaf(b0, cj, a0 * sj);
           }
         }
       }

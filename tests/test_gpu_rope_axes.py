@@ -292,3 +292,36 @@ def test_refusals(qa):
     with pytest.raises(qa.QmAttnError) as e:
         qa.qk_norm_rope(q, k, positions=at, axes=[], layout="bnhd")   # no rotation
     assert e.value.status == qa.QM_ERR_ROTARY
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("layout", ["bnhd", "bhnd"])
+@pytest.mark.parametrize("dtype", ["float16", "bfloat16"])
+@pytest.mark.parametrize("d,N", [(128, 40), (128, 750), (64, 1500), (128, 2000)])
+def test_one_rotation_whatever_the_call(qa, d, N, dtype, layout, interleaved):
+    """The same keys and queries at the same positions give the same bytes from the call of one
+    axis and from that of several, and with or without a cache: in small calls, in large
+    ones, and in those that are large for the values that they cache alone."""
+    import torch
+    H, Hkv, page = 32, 8, 16
+    dtype = getattr(torch, dtype)
+    q, k, v = _inputs(1, N, H, Hkv, d, dtype, layout, 50)
+    cos, sin = so.rotation_table(N + 7, d)
+    w = (1 + 0.3 * torch.randn(d, generator=_gen(51), device="cuda")).to(dtype)
+    starts = torch.tensor([7], dtype=torch.int32, device="cuda")
+    table = torch.randperm((N + 7 + page - 1) // page, generator=_gen(52), device="cuda").to(torch.int32)[None]
+    positions = (7 + torch.arange(N, device="cuda", dtype=torch.int32)).expand(3, 1, N).contiguous()
+    results = []
+    for place in (dict(starts=starts), dict(positions=positions[:1]), dict(positions=positions, axes=_axes_of("turns", d // 2, 3)),
+                  dict(positions=positions, axes=_axes_of("runs", d // 2, 3))):
+        kw = dict(cos=cos, sin=sin, q_weight=w, k_weight=w, layout=layout, interleaved=interleaved)
+        plain = qa.qk_norm_rope(q, k, **kw, **place)
+        caches = [torch.zeros(table.shape[1], Hkv, page, d, device="cuda", dtype=dtype) for _ in range(2)]
+        k_out = torch.empty(k.shape, device="cuda", dtype=dtype)
+        q_out = qa.qk_norm_rope_append(q, k, v, *caches, table, k_out=k_out, **kw, **dict(place, starts=starts))
+        results.append([*plain, q_out, k_out, *caches])
+    first = results[0]
+    assert torch.equal(_bits(first[0]), _bits(first[2])) and torch.equal(_bits(first[1]), _bits(first[3]))
+    for got in results[1:]:
+        for i, (a, b) in enumerate(zip(got, first)):
+            assert torch.equal(_bits(a), _bits(b)), i
