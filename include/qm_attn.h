@@ -102,8 +102,8 @@ enum {
   QM_ERR_WORKSPACE = -16,  /* workspace is NULL or smaller than the call needs */
   QM_ERR_NORM = -17,       /* qm_rms_norm: width is not a multiple of 8 from 8 to 32768 (and of
                               group, which is 0, 32, 64, 128 or 256), or eps not finite or below 0 */
-  QM_ERR_AXES = -18        /* positions of several axes: axes not from 1 to 4, a pair's axis not
-                              below axes, or starts given to a call that writes no cache */
+  QM_ERR_AXES = -18        /* positions of several axes: axes not from 1 to 4, or a pair's axis not
+                              below axes */
 };
 
 /*
@@ -448,7 +448,9 @@ int qm_qk_norm_rope_append_axes(
  *                      a residual only (QM_ERR_NULL).
  *   width        a multiple of 8 from 8 to 32768 (QM_ERR_NORM).     rows   1 or more.
  *   A row whose mean square overflows fp32 has y = 0; one that holds a NaN or an infinity
- *   has NaN in y, there at least.  Other rows are not affected.
+ *   has NaN in y, there at least.  With eps = 0 a row of zeros has NaN, and one whose mean
+ *   square is below 2^-126 (values of 10^-19) has an inexact y, infinities or NaN.  Other rows
+ *   are not affected.
  *   stream, errors, capture: as for the calls above (one kernel, or, of more than 2^21 rows,
  *   one for each 2^21 at least; nothing else).
  */
