@@ -14,14 +14,9 @@ namespace qm {
 namespace {
 
 constexpr int kBlock = kDecodeBlock;   // tokens of a wavefront's step
-constexpr int kMinShare = 4;           // least blocks of a workgroup's share: one a wavefront
 // The second product's factor (see decode.hip); O is divided by it at the end.
 template <int DT>
 constexpr float kWeight = DT == 0 ? 32768.f : 1.f;
-// What a row costs a workgroup beside its blocks, in blocks: its first loads and its
-// join, 5-8 us, against 1.1 us a block.  Counted as 0, 6 and 12 (us): 512 rows of up to
-// 8192 tokens 205, 198, 199; up to 2000 88, 64, 65; 8 rows of 2000 13.4, 10.8, 10.8.
-constexpr int kRowCost = 6;
 
 struct Params {
   const uint16_t* q;

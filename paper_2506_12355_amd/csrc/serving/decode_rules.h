@@ -9,6 +9,11 @@
 namespace qm {
 
 constexpr int kDecodeBlock = 32;   // tokens of a wavefront's step
+constexpr int kMinShare = 4;       // least blocks of a workgroup's share: one a wavefront
+// What a row costs a workgroup beside its blocks, in blocks: its first loads and its
+// join, 5-8 us, against 1.1 us a block.  Counted as 0, 6 and 12 (us): 512 rows of up to
+// 8192 tokens 205, 198, 199; up to 2000 88, 64, 65; 8 rows of 2000 13.4, 10.8, 10.8.
+constexpr int kRowCost = 6;
 
 // Most 32-token blocks that hold visible tokens of a sequence of up to `limit`: those
 // of the first keys, and those of a window that begins and ends inside a block.

@@ -353,7 +353,7 @@ __device__ __forceinline__ void load_to_lds(const uint8_t* base, uint32_t from, 
 }
 
 // A part of the prefix for one tile of 128 rows, 32 a wavefront: the wavefronts walk its
-// blocks together through rings in LDS of three blocks of keys and three of values, which
+// blocks together through rings in LDS of three blocks of keys and three of values,
 // whose loads go out two steps before they are read: from memory straight into LDS, or, of
 // E4M3 codes, through registers, where they are widened.
 template <int DT, int D, bool FP8>

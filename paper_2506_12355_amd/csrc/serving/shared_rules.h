@@ -51,7 +51,7 @@ inline SharedPlan plan_shared(int64_t B, int64_t H, int64_t Hkv, int d, int es, 
   p.splits = (int)splits;
   // eight (head, part) pairs side by side, one to an XCD, each with all of its tiles
   p.prefix_grid = (int)((Hkv * splits + 7) / 8 * 8 * tiles);
-  const int64_t shares = (own_rows * (own_blocks + 6) + 3) / 4;
+  const int64_t shares = (own_rows * (own_blocks + kRowCost) + kMinShare - 1) / kMinShare;   // as share_of deals them
   p.join_threads = B * H < 4 * (int64_t)cus ? 256 : 64;
   // Beside few rows, own tokens' workgroups are those that are on the device with the prefix's, one a
   // CU at least (us, and with two a CU: 8 sequences 4000 + 1000 17.5, 21.6, + 4000 22.4, 27.2).  Beside
