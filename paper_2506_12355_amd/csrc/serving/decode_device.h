@@ -378,7 +378,7 @@ __device__ __forceinline__ int running_sum(int x) {
 
 // Equal shares of all rows' blocks: that of workgroup `own` of `grid`.
 template <int DT, int D, bool FP8, bool OWN>
-__device__ __forceinline__ void share_of(const Params& p, float* lds, int own, int grid) {
+__device__ __forceinline__ void share_of(const Params& p, float* lds, uint32_t own, uint32_t grid) {
   constexpr int WAVES = 4;
   const int rows = p.Hkv * p.tiles;   // of a sequence
   const int lane = threadIdx.x & 63;

@@ -35,8 +35,6 @@ struct Stream {
   int64_t sb, sn, sh;     // input strides, elements
   FastDiv inner, outer;   // of a row index, in the order of the output
   uint32_t rows, units;
-  FastDiv blocks, head_blocks;   // of a unit's index, where a lane has several heads
-  uint32_t batches;
   float inv;              // cached values are multiplied by this
 };
 
@@ -50,12 +48,19 @@ struct Params {
   FastDiv page;
   int rotary, table_rows, interleaved, bnhd;
   float eps;
-  // positions of several axes
+};
+
+// With positions of several axes.  (A struct of its own: calls of one axis, which are short,
+// take no arguments that they do not read.)
+struct AxesParams : Params {
   const int32_t* positions;
   int64_t axis_stride;
-  int N, used_axes;
+  int B, N, used_axes;
   uint64_t pair_axis[2];
+  FastDiv blocks[3], head_blocks[3];   // of a unit's index in q, k and v, where a lane has several heads
 };
+template <bool AXES>
+using ParamsOf = std::conditional_t<AXES, AxesParams, Params>;
 
 // Sum over the L (4 or 8) neighbouring lanes that hold a row.
 template <int L>
@@ -72,7 +77,7 @@ __device__ __forceinline__ float row_sum(float x) {
 
 // The rows of one unit of q (KIND 0), k (1) or v (2).
 template <int DT, int D, bool AXES, int HEADS, int KIND>
-__device__ __forceinline__ void unit_rows(const Params& p, const Stream& s, uint32_t unit) {
+__device__ __forceinline__ void unit_rows(const ParamsOf<AXES>& p, const Stream& s, uint32_t unit) {
   using T = Type16<DT>;
   constexpr int L = D / 16;      // lanes of a row
   constexpr int R = 64 / L;      // rows of a wavefront at once
@@ -93,20 +98,21 @@ __device__ __forceinline__ void unit_rows(const Params& p, const Stream& s, uint
 
   uint32_t row = unit * R + lane / L, b, h, t;
   const uint32_t heads = p.bnhd ? s.inner.d : s.outer.d;
-  if (HEADS > 1) {
+  if constexpr (HEADS > 1) {
+    const FastDiv &blocks = p.blocks[KIND], &head_blocks = p.head_blocks[KIND];
     // a lane's rows: of one token, HEADS heads, R apart (a wavefront has R * HEADS of a token) or
     // neighbours (it has those of R tokens)
-    const uint32_t token = p.bnhd ? s.blocks.div(unit) : 0, block = p.bnhd ? unit - token * s.blocks.d : s.blocks.div(unit);
+    const uint32_t token = p.bnhd ? blocks.div(unit) : 0, block = p.bnhd ? unit - token * blocks.d : blocks.div(unit);
     if (p.bnhd) {
       b = s.outer.div(token);
       t = token - b * s.outer.d;
       h = block * (R * HEADS) + lane / L;
     } else {   // blocks of R tokens the inner index, blocks of HEADS heads the next
-      t = (unit - block * s.blocks.d) * R + lane / L;
-      b = s.head_blocks.div(block);
-      h = (block - b * s.head_blocks.d) * HEADS;
+      t = (unit - block * blocks.d) * R + lane / L;
+      b = head_blocks.div(block);
+      h = (block - b * head_blocks.d) * HEADS;
     }
-    if (b >= s.batches || h >= heads || t >= (uint32_t)p.N) return;
+    if (b >= (uint32_t)p.B || h >= heads || t >= (uint32_t)p.N) return;
   } else if (row >= s.rows) {
     return;
   } else if (p.bnhd) {
@@ -124,7 +130,7 @@ __device__ __forceinline__ void unit_rows(const Params& p, const Stream& s, uint
   const bool held = !p.counts || (int)t < p.counts[b];
   bool fits = !p.rotary || (at >= 0 && at < p.table_rows);
   int row0 = 0, row1 = 0, row2 = 0, row3 = 0;   // the token's row of the table on each axis
-  if (AXES && held) {
+  if constexpr (AXES) if (held) {
     const int32_t* own = p.positions + (int64_t)b * p.N + t;
     if (p.used_axes & 1) row0 = own[0];
     if (p.used_axes & 2) row1 = own[p.axis_stride];
@@ -138,7 +144,7 @@ __device__ __forceinline__ void unit_rows(const Params& p, const Stream& s, uint
   auto load_angles = [&]() __attribute__((always_inline)) {
     int64_t line = at;
     bool one = true;   // the lane's pairs lie in one row of the table
-    if (AXES) {
+    if constexpr (AXES) {
       // the axes of pairs 8 i .. 8 i + 7
       const uint32_t of = (uint32_t)(p.pair_axis[i >= 4] >> (16 * (i & 3))) & 0xffffu;
       auto row_of = [&](uint32_t a) __attribute__((always_inline)) {
@@ -255,7 +261,7 @@ __device__ __forceinline__ void unit_rows(const Params& p, const Stream& s, uint
       }
     }
   };
-  if (HEADS == 1) {
+  if constexpr (HEADS == 1) {
     one_row(row, h);
   } else {
     if (held && turned && fits) load_angles();
@@ -267,7 +273,7 @@ __device__ __forceinline__ void unit_rows(const Params& p, const Stream& s, uint
 }
 
 template <int DT, int D, bool AXES, int HEADS>
-__global__ __launch_bounds__(256) void norm_rope_kernel(Params p) {
+__global__ __launch_bounds__(256) void norm_rope_kernel(ParamsOf<AXES> p) {
   uint32_t unit = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
   if (unit < p.s[0].units) return unit_rows<DT, D, AXES, HEADS, 0>(p, p.s[0], unit);
   unit -= p.s[0].units;
@@ -286,7 +292,7 @@ constexpr int kHeads = 4;
 template <int DT, int D>
 hipError_t launch(const NormRopeArgs& a, hipStream_t stream) {
   constexpr int kRows = 64 / (D / 16);   // rows of a wavefront
-  Params p = {};
+  AxesParams p = {};
   const uint16_t* in[3] = {a.q, a.k, a.v};
   uint16_t* out[3] = {a.q_out, a.k_out, nullptr};
   uint32_t units = 0;
@@ -318,7 +324,7 @@ hipError_t launch(const NormRopeArgs& a, hipStream_t stream) {
   if (a.positions) {
     p.positions = a.positions;
     p.axis_stride = (int64_t)a.B * a.N;
-    p.N = a.N, p.used_axes = a.used_axes;
+    p.B = a.B, p.N = a.N, p.used_axes = a.used_axes;
     p.pair_axis[0] = a.pair_axis[0], p.pair_axis[1] = a.pair_axis[1];
     // (blocks of rows of one token, or of one head, that would not fill a wavefront, and
     // launches of few wavefronts, keep one row a lane)
@@ -331,9 +337,8 @@ hipError_t launch(const NormRopeArgs& a, hipStream_t stream) {
         const int heads = i == 0 ? a.H : a.Hkv;
         const uint32_t token_blocks = (a.N + kRows - 1) / kRows, per = a.layout ? kRows * kHeads : kHeads;
         const uint32_t head_blocks = (heads + per - 1) / per;
-        s.blocks = FastDiv(a.layout ? head_blocks : token_blocks);
-        s.head_blocks = FastDiv(head_blocks);
-        s.batches = a.B;
+        p.blocks[i] = FastDiv(a.layout ? head_blocks : token_blocks);
+        p.head_blocks[i] = FastDiv(head_blocks);
         s.units = (uint32_t)((int64_t)a.B * head_blocks * (a.layout ? a.N : token_blocks));
         units += s.units;
       }
@@ -343,7 +348,8 @@ hipError_t launch(const NormRopeArgs& a, hipStream_t stream) {
     hipLaunchKernelGGL((norm_rope_kernel<DT, D, true, 1>), dim3((units + 3) / 4), dim3(256), 0, stream, p);
     return hipGetLastError();
   }
-  hipLaunchKernelGGL((norm_rope_kernel<DT, D, false, 1>), dim3((units + 3) / 4), dim3(256), 0, stream, p);
+  hipLaunchKernelGGL((norm_rope_kernel<DT, D, false, 1>), dim3((units + 3) / 4), dim3(256), 0, stream,
+                     static_cast<const Params&>(p));
   return hipGetLastError();
 }
 
