@@ -16,10 +16,10 @@
 // one stream; several rows in turn, angles and weights kept, were slower (two and four
 // rows a lane, below).
 //
-// Measured (us, bf16, d = 128, a plain copy runs at 5.24 TB/s): 72 heads of 8192 tokens
-// 58.9 (5.2 TB/s; two and four rows a lane 4% and 8% more), head-major 62.5; one token
-// 3.2 (3.9, 5.9); 4 ragged prompts of up to 2000 tokens into E4M3 pages 29-31
-// (4.7-5.0 TB/s), into bf16 ones 31.7 (5.0).
+// Measured (us, bf16, d = 128, over more inputs than the last-level cache holds; a plain copy runs
+// at 5.1 TB/s): 72 heads of 8192 tokens 55-58 (5.2-5.5 TB/s; two and four rows a lane 4% and 8%
+// more), head-major 61; one token 2.9 (two and four rows a lane 0.7 and 2.7 more); 4 ragged
+// prompts of up to 2000 tokens into E4M3 pages 30-31 (4.7-4.9 TB/s), into bf16 ones 31.6 (5.0).
 #include "serving_device.h"
 #include "serving_launch.h"
 
@@ -282,11 +282,14 @@ __global__ __launch_bounds__(256) void norm_rope_kernel(ParamsOf<AXES> p) {
   if (unit < p.s[2].units) unit_rows<DT, D, AXES, HEADS, 2>(p, p.s[2], unit);
 }
 
-// With positions of several axes a lane takes four heads of its token, so that the angles,
-// which lie in up to eight places of the table for its eight pairs, are fetched once for
-// them (us, one, two, four and eight heads; axes in turn over the pairs: 4 prompts of up to
-// 1999 tokens into E4M3 pages 53.1, 36.9, 32.9, 33.7, 72 heads of 8192 tokens 98.7, 74.5, 63.3,
-// 60.7; a run of pairs each: 28.0, 26.9, 26.9, 28.4 and 60.5, 60.3, 55.5, 54.9).
+// With positions of several axes a lane takes four heads of its token in large calls, so that the
+// angles, which lie in up to eight places of the table for its eight pairs, are fetched once
+// for them (us, one, two, four and eight heads, over more inputs than the last-level cache holds;
+// axes in turn over the pairs: 4 prompts of up to 1999 tokens into E4M3 pages 59.5, 45.8, 39.9,
+// 40.9, 72 heads of 8192 tokens 96.5, 68.7, 63.8, 62.3; a run of pairs each: 35.1, 33.5, 31.3, 31.8
+// and 61.6, 57.6, 58.3, 57.7).  Large: of 4096 wavefronts on (us, 32/8 heads, one and four heads a
+// lane, axes in turn, token-major, and in runs: 400 tokens, 2000 wavefronts, 7.0, 9.4 and 5.6, 8.7;
+// 800 9.9, 10.5 and 7.1, 9.4; 1600 15.8, 12.6 and 10.7, 10.4; 3200 27.6, 21.1 and 17.9, 16.2).
 constexpr int kHeads = 4;
 
 template <int DT, int D>
@@ -327,7 +330,7 @@ hipError_t launch(const NormRopeArgs& a, hipStream_t stream) {
     p.B = a.B, p.N = a.N, p.used_axes = a.used_axes;
     p.pair_axis[0] = a.pair_axis[0], p.pair_axis[1] = a.pair_axis[1];
     // (blocks of rows of one token, or of one head, that would not fill a wavefront, and
-    // launches of few wavefronts, keep one row a lane)
+    // launches of few wavefronts, keep one row a lane: see kHeads)
     const bool blocks = a.layout ? a.Hkv >= kRows && a.H >= kRows : a.N >= kRows;
     if (blocks && units >= 1024u * kHeads) {
       units = 0;

@@ -23,8 +23,8 @@
 // as far off as a result rounded once; on the matrix cores that is half as many products again.
 //
 // Measured (us, bf16, d = 128, 64/8 heads, no own tokens, with the join): 64 sequences behind
-// 8192 tokens 46.5, behind 32768 121 (2.9 us a 1024 tokens: 720 TFLOP/s, 1080 of products); in
-// prefix_piece alone 56 and 171.
+// 8192 tokens 43.3, behind 32768 103.9 (2.5 us a 1024 tokens: 850 TFLOP/s, 1275 of products); in
+// prefix_piece alone 56.5 and 173.5.
 #include "decode_device.h"
 #include "shared_rules.h"
 
