@@ -42,14 +42,16 @@ namespace {
 // of them, a lane's, sum to more than kMostWeight (always in a row's first block): a step's
 // weights then wait for no maximum, and the accumulators are scaled in few steps.  A row is
 // redone by its own weights alone, so that what its neighbours hold changes none of its bits;
-// then 32 rows have a step each, and room of 8 is too little (us, 64 sequences of 64/8 heads
-// behind 32768 tokens: bf16 8 117, 64 104.5, 1024 104.9; d = 64 78.7, 67.6, 67.2; E4M3 119, 106.7,
-// 105.6; f16 8 124, 16 115.5, 32 115.0).  bf16 has fp32's exponents; f16's factor brings the largest
-// weights to 2^15, so that of those far below a row's largest 2^-36 each is lost.
+// then each of 32 rows has steps of its own, and room is what keeps them few (us, 64 sequences of
+// 64/8 heads behind 32768 tokens, scores of a standard deviation of 1, 3 and 6: bf16, room 1024
+// 110, 111, 124, 65536 107, 108, 116; E4M3 behind 65500 73, 73, 83, 72, 72, 76; f16, room 16 118, 131,
+// 134, 256 117, 122, 127; with room 8, spread 1, bf16 117 where 1024 has 105).  bf16 has fp32's
+// exponents; f16's factor brings the largest weights to 2^15, so that of those far below a
+// row's largest 2^-32 each is lost: with 65536 tokens 2^-16 of their values.
 template <int DT>
-constexpr float kMostWeight = DT == 0 ? 16.f : 1024.f;
+constexpr float kMostWeight = DT == 0 ? 256.f : 65536.f;
 template <int DT>
-constexpr float kFactor = DT == 0 ? 2048.f : 1.f;
+constexpr float kFactor = DT == 0 ? 128.f : 1.f;
 
 // a - the low half of w, b - the high half: what rounding a and b into w left, exactly.  (The
 // factors stand in registers: written as constants, -1 in the low half is compiled into the
