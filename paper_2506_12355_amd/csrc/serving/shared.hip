@@ -23,8 +23,8 @@
 // as far off as a result rounded once; on the matrix cores that is half as many products again.
 //
 // Measured (us, bf16, d = 128, 64/8 heads, no own tokens, with the join): 64 sequences behind
-// 8192 tokens 43.3, behind 32768 103.9 (2.5 us a 1024 tokens: 850 TFLOP/s, 1275 of products); in
-// prefix_piece alone 56.5 and 173.5.
+// 8192 tokens 44.2, behind 32768 108.4 (2.7 us a 1024 tokens: 800 TFLOP/s, 1200 of products); in
+// prefix_piece alone 58.7 and 179.
 #include "decode_device.h"
 #include "shared_rules.h"
 

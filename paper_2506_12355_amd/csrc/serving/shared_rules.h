@@ -42,9 +42,9 @@ inline SharedPlan plan_shared(int64_t B, int64_t H, int64_t Hkv, int d, int es, 
   // is a block of own tokens of 16 KB; of their most, half is counted, as lengths vary).  Few
   // rows, which wait for memory, take one by the same rule, a tile's block as half a unit.
   // us, two and one, 64/8 heads, the prefix's tokens and the most own ones: 64 sequences
-  // 8192 + 64 54.3, 46.8, + 500 61.1, 50.0, + 8000 244, 215; 32768 + 64 107, 126, + 8000 293, 232; of E4M3
-  // 32768 + 2000 135, 138, + 8000 215, 161; d = 64 8192 + 2000 49.4, 43.1, 32768 + 2000 78.1, 96.6;
-  // 8 sequences 16384 + 300 34.5, 30.2, 65536 + 300 68.0, 69.4, d = 64 41.7, 51.6.
+  // 8192 + 64 55.6, 48.8, + 500 61.5, 50.9, + 8000 243, 215; 32768 + 64 112, 129, + 8000 294, 231; of E4M3
+  // 32768 + 2000 145, 149, + 8000 221, 171; d = 64 8192 + 2000 51.3, 43.4, 32768 + 2000 82.8, 100;
+  // 8 sequences 16384 + 300 34.5, 30.4, 65536 + 300 69.6, 71.5, d = 64 41.3, 51.6.
   const double prefix_work = (double)(Hkv * tiles * blocks) * (p.rt == 8 ? 1.0 : 0.5) * (d == 128 ? 1.0 : 0.65);
   const double own_work = (double)(own_rows * own_blocks) * (d * es / 256.0), saved = 7600.0 * d / 128;
   const bool beside = own_blocks && prefix_work < own_work + saved;
